@@ -280,6 +280,120 @@ stage_status stage_lm_head(stage_t* st, const void* final_norm, const void* w_lm
 stage_status stage_pack_lm_head(const stage_model_config* cfg, int32_t vocab, const void* src,
                                 void* dst, void* stream);
 
+/* ---- 8-bit products ----------------------------------------------------- */
+/* out = a b^T with both operands in 8-bit integers and a float32 scale for
+ * each row of either: per token of the activations a [m, k], per channel of
+ * the weights b [n, k]. Half the weight bytes of bf16, which is what bounds a
+ * decode step's products (Table 2; Sec. 2.3, memory-bound decode).
+ *  - A quantised matrix is opaque device memory of stage_quant_bytes(rows, k)
+ *    bytes, 16-byte aligned, written by stage_quant_rows or stage_quant_pack:
+ *    operand fragments of the 8-bit matrix instructions, then the scales.
+ *    Activations and weights have the same form. It belongs to its (rows, k):
+ *    a product must name the ones that it was made with.
+ *  - quant_rows: scale s = max(max |x| / 127, 2^-120) of the row, value
+ *    rint(x * (1 / s)), each step rounded to nearest in float32. A row that
+ *    holds a NaN or an infinity makes its row (for weights: column) of every
+ *    product NaN, and no other.
+ *  - Sums are exact (int32; k <= 131072, else STAGE_ERR_UNSUPPORTED); then
+ *    out = sum * (scale_a * scale_b) in float32, rounded once to out_dtype.
+ *  - Any rows, k and n from 1 on (rows or n 0: nothing is done); row strides
+ *    (ld, in elements, >= the row's length) and addresses as the types allow.
+ *    Output and inputs must not overlap.
+ *  - These calls, and those of the next section, need no stage: they run on the
+ *    current device, whose memory their pointers name and whose stream `stream`
+ *    is. They keep nothing between calls and may be captured into a graph. */
+
+/* Bytes of a quantised [rows, k] matrix; 0 if the size is not supported. */
+size_t stage_quant_bytes(int32_t rows, int32_t k);
+
+/* Quantise a row-major [rows, k] matrix of `dtype` into dst: the activations
+ * of a product, or (once, when it is loaded) its weights. */
+stage_status stage_quant_rows(stage_dtype dtype, const void* src, int64_t ld, int32_t rows,
+                              int32_t k, void* dst, void* stream);
+
+/* Bring int8 values [rows, k] with scales [rows] (float32, device) that the
+ * caller has, e.g. weights quantised when the model was made, into dst. */
+stage_status stage_quant_pack(const int8_t* src, int64_t ld, const float* scales, int32_t rows,
+                              int32_t k, void* dst, void* stream);
+
+/* out [m, n] (row-major, stride ldo) = a b^T of two quantised matrices. */
+stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_t n, int32_t k,
+                                 stage_dtype out_dtype, void* out, int64_t ldo, void* stream);
+
+/* stage_lm_head with W_lm as a quantised [vocab, hidden] matrix: the normed
+ * rows are quantised from float32 (they are not rounded to the mode dtype
+ * first). Any vocab >= 1; everything else as for stage_lm_head, the pointers
+ * hidden and final_norm 16-byte aligned. */
+stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void* w_lm,
+                                 int32_t vocab, const void* hidden, int32_t hidden_rows,
+                                 const int32_t* rows, int32_t n_rows, float* logits,
+                                 void* stream);
+
+/* ---- from logits to tokens ---------------------------------------------- */
+/* probs[r] = softmax(logits[r] / temperature[r]) over vocab tokens.
+ *  logits:      device [rows, vocab] of `dtype`, row stride ld, e.g. what
+ *               stage_lm_head wrote. A token is masked out by -infinity.
+ *  temperature: device float32 [rows], or NULL for 1 throughout. One that is
+ *               not above 2^-100 (0, negative, NaN) puts 1 on the largest logit,
+ *               the lowest token among equals, and 0 elsewhere; above 2^100 it
+ *               counts as 2^100.
+ *  probs:       device [rows, vocab] of out_dtype, row stride ld_out. May be the
+ *               logits themselves (same type and stride); must not overlap them
+ *               otherwise.
+ *  ws:          device scratch of stage_token_probs_bytes() bytes, 16-byte
+ *               aligned; nothing in it needs initialising.
+ * Sums are float32. A row whose tokens are all masked gets zeros; a row with a
+ * NaN or +infinity gets NaN throughout. */
+size_t stage_token_probs_bytes(int32_t rows, int32_t vocab);
+stage_status stage_token_probs(stage_dtype dtype, const void* logits, int64_t ld, int32_t rows,
+                               int32_t vocab, const float* temperature, stage_dtype out_dtype,
+                               void* probs, int64_t ld_out, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/* Drafted tokens to verify. Sequence i has the drafts starts[i] ..
+ * starts[i + 1] - 1 (none, or at most max_drafts); the target's rows of a
+ * sequence follow each other, one for each draft and one for the token after
+ * the last: row starts[i] + i + j holds the probabilities of its j-th new token.
+ * All arrays are device memory. */
+typedef struct {
+  stage_dtype dtype;         /* of both sets of probabilities */
+  int32_t vocab;
+  int32_t num_seqs;          /* at most 65535 */
+  int32_t num_drafts;        /* of all sequences: starts[num_seqs] */
+  int32_t max_drafts;        /* of one sequence */
+  const void* target_probs;  /* [num_drafts + num_seqs, vocab], row stride ld_target */
+  int64_t ld_target;
+  const void* draft_probs;   /* [num_drafts, vocab], row stride ld_draft: what each
+                                draft was drawn from; NULL: chosen outright (as by
+                                a table look-up), probability 1 */
+  int64_t ld_draft;
+  const int32_t* drafts;     /* [num_drafts] token ids */
+  const int32_t* starts;     /* [num_seqs + 1], from 0, non-decreasing */
+  const float* accept_u;     /* [num_drafts] uniform random numbers in [0, 1) */
+  const float* sample_u;     /* [num_seqs] likewise */
+} stage_drafts;
+
+/* Verify drafts against the target model's probabilities so that the tokens
+ * are distributed as if the target had drawn them one by one. Draft j with
+ * token d is accepted while all before it are and u_j q_j(d) < p_j(d). The
+ * token after the accepted ones is drawn from max(p - q, 0) of the refused
+ * position (with p itself if nothing is left of it), or from the last row if
+ * all are accepted: the lowest token t with w_0 + .. + w_t > sample_u * (the
+ * sum of all w), products and sums in float64. Weights that are not positive
+ * and finite count as 0; probabilities need not sum to 1.
+ *  n_accepted: device int32 [num_seqs], written.
+ *  tokens:     device int32 [num_seqs][max_drafts + 1], written: the accepted
+ *              drafts, the drawn token, then -1. The drawn token is -1 if its
+ *              row has no positive weight.
+ *  ws:         device scratch of stage_verify_bytes() bytes, 16-byte aligned;
+ *              nothing in it needs initialising.
+ * Offsets in starts are clamped to [0, num_drafts] and to max_drafts per
+ * sequence, and a draft outside [0, vocab) is refused: no read leaves the
+ * arrays whatever the device arrays hold. */
+size_t stage_verify_bytes(int32_t num_seqs, int32_t vocab);
+stage_status stage_verify_drafts(const stage_drafts* drafts, int32_t* n_accepted, int32_t* tokens,
+                                 void* ws, size_t ws_bytes, void* stream);
+
 /* ---- shared tensor store ---------------------------------------------- */
 /* The paper keeps model weights and KV-cache space in a store process that
  * loads them once and hands them to engine processes zero-copy, so that an

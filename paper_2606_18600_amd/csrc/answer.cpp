@@ -1,0 +1,235 @@
+// The C ABI of the answer operators: 8-bit products, the LM head on them, token
+// probabilities and draft verification (include/stage.h). Arguments are checked
+// here, before anything is enqueued.
+#include <hip/hip_runtime.h>
+
+#include <cstdarg>
+#include <cstdio>
+
+#include "../../include/stage.h"
+#include "answer.hpp"
+#include "lm_head.hpp"
+
+using namespace stage_k;
+
+namespace {
+
+constexpr int64_t kMaxLd = (int64_t)1 << 40;  // row offsets stay far below 2^63
+constexpr int kMaxQuantRows = 1 << 24;
+constexpr int kMaxSeqs = 65535;  // a grid dimension
+constexpr int kMaxVocab = 1 << 30;
+
+stage_status op_fail(stage_status code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  set_error(buf);
+  return code;
+}
+
+stage_status launched(const char* what, hipError_t e) {
+  if (e == hipSuccess) return STAGE_OK;
+  return op_fail(STAGE_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+bool is_dtype(int d) { return d == STAGE_F32 || d == STAGE_BF16; }
+
+bool at_multiple(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
+
+size_t esize(int d) { return d == STAGE_F32 ? 4 : 2; }
+
+// A quantised matrix's size, as every call checks it.
+stage_status check_matrix(int32_t rows, int32_t k, const char* what) {
+  if (rows < 0 || k < 1)
+    return op_fail(STAGE_ERR_INVALID_ARG, "%s: %d rows of %d values", what, rows, k);
+  if (k > kQuantMaxK)
+    return op_fail(STAGE_ERR_UNSUPPORTED, "%s: %d values per row > %d (int32 sums)", what, k,
+                   kQuantMaxK);
+  if (rows > kMaxQuantRows)
+    return op_fail(STAGE_ERR_UNSUPPORTED, "%s: %d rows > %d", what, rows, kMaxQuantRows);
+  return STAGE_OK;
+}
+
+// A row-major [rows, cols] matrix of the caller.
+stage_status check_rows(const void* p, int64_t ld, int32_t cols, size_t es, const char* what) {
+  if (!p) return op_fail(STAGE_ERR_INVALID_ARG, "%s is NULL", what);
+  if (!at_multiple(p, es))
+    return op_fail(STAGE_ERR_INVALID_ARG, "%s is not aligned to its type", what);
+  if (ld < cols || ld > kMaxLd)
+    return op_fail(STAGE_ERR_INVALID_ARG, "%s: row stride %lld for rows of %d", what,
+                   (long long)ld, cols);
+  return STAGE_OK;
+}
+
+stage_status check_packed(const void* p, const char* what) {
+  if (!p) return op_fail(STAGE_ERR_INVALID_ARG, "%s is NULL", what);
+  if (!at_multiple(p, 16)) return op_fail(STAGE_ERR_INVALID_ARG, "%s not 16-byte aligned", what);
+  return STAGE_OK;
+}
+
+stage_status check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return STAGE_OK;
+  if (!ws) return op_fail(STAGE_ERR_INVALID_ARG, "workspace is NULL");
+  if (bytes < need)
+    return op_fail(STAGE_ERR_CAPACITY, "workspace of %zu bytes < required %zu", bytes, need);
+  if (!at_multiple(ws, 16)) return op_fail(STAGE_ERR_INVALID_ARG, "workspace not 16-byte aligned");
+  return STAGE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t stage_quant_bytes(int32_t rows, int32_t k) {
+  return check_matrix(rows, k, "quantised matrix") == STAGE_OK ? quant_bytes(rows, k) : 0;
+}
+
+stage_status stage_quant_rows(stage_dtype dtype, const void* src, int64_t ld, int32_t rows,
+                              int32_t k, void* dst, void* stream) {
+  const int d = (int)dtype;
+  if (!is_dtype(d)) return op_fail(STAGE_ERR_UNSUPPORTED, "dtype %d not supported", d);
+  stage_status v = check_matrix(rows, k, "quant_rows");
+  if (v != STAGE_OK || rows == 0) return v;
+  if ((v = check_rows(src, ld, k, esize(d), "src")) != STAGE_OK) return v;
+  if ((v = check_packed(dst, "dst")) != STAGE_OK) return v;
+  return launched("quant_rows", quant_rows((DType)d, src, ld, rows, k, dst, (hipStream_t)stream));
+}
+
+stage_status stage_quant_pack(const int8_t* src, int64_t ld, const float* scales, int32_t rows,
+                              int32_t k, void* dst, void* stream) {
+  stage_status v = check_matrix(rows, k, "quant_pack");
+  if (v != STAGE_OK || rows == 0) return v;
+  if ((v = check_rows(src, ld, k, 1, "src")) != STAGE_OK) return v;
+  if (!scales || !at_multiple(scales, 4))
+    return op_fail(STAGE_ERR_INVALID_ARG, "scales is NULL or not aligned to its type");
+  if ((v = check_packed(dst, "dst")) != STAGE_OK) return v;
+  return launched("quant_pack", quant_pack(src, ld, scales, rows, k, dst, (hipStream_t)stream));
+}
+
+stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_t n, int32_t k,
+                                 stage_dtype out_dtype, void* out, int64_t ldo, void* stream) {
+  const int d = (int)out_dtype;
+  if (!is_dtype(d)) return op_fail(STAGE_ERR_UNSUPPORTED, "dtype %d not supported", d);
+  stage_status v = check_matrix(m, k, "a");
+  if (v != STAGE_OK) return v;
+  if ((v = check_matrix(n, k, "b")) != STAGE_OK) return v;
+  if (m == 0 || n == 0) return STAGE_OK;
+  if ((v = check_packed(a, "a")) != STAGE_OK) return v;
+  if ((v = check_packed(b, "b")) != STAGE_OK) return v;
+  if ((v = check_rows(out, ldo, n, esize(d), "out")) != STAGE_OK) return v;
+  return launched("quant_product",
+                  quant_product(a, m, b, n, k, (DType)d, out, ldo, (hipStream_t)stream));
+}
+
+stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void* w_lm,
+                                 int32_t vocab, const void* hidden, int32_t hidden_rows,
+                                 const int32_t* rows, int32_t n_rows, float* logits,
+                                 void* stream) {
+  if (!at_multiple(w_lm, 16) || !at_multiple(hidden, 16) || !at_multiple(final_norm, 16) ||
+      !at_multiple(logits, 4))
+    return op_fail(STAGE_ERR_INVALID_ARG, "w_lm/hidden/final_norm/logits is not aligned");
+  if (vocab > kMaxQuantRows)
+    return op_fail(STAGE_ERR_UNSUPPORTED, "vocab %d > %d", vocab, kMaxQuantRows);
+  LmHeadProduct f;
+  f.norm = [](const LmHeadProduct&, const LmHeadRows& r, hipStream_t s) {
+    if (quant_bytes(r.n, r.H) > r.h_bytes) return hipErrorInvalidValue;
+    return quant_norm_rows(r.dt, r.hidden, r.idx, r.gain, r.eps, r.n, r.H, r.h, s);
+  };
+  f.product = [](const LmHeadProduct& p, const LmHeadRows& r, hipStream_t s) {
+    return quant_product(r.h, r.n, p.w, p.vocab, r.H, DT_F32, p.logits, p.vocab, s);
+  };
+  f.w = w_lm;
+  f.vocab = vocab;
+  f.logits = logits;
+  return lm_head_rows(st, f, final_norm, hidden, hidden_rows, rows, n_rows, stream);
+}
+
+size_t stage_token_probs_bytes(int32_t rows, int32_t vocab) {
+  return rows < 0 || vocab < 1 || vocab > kMaxVocab ? 0 : token_probs_bytes(rows, vocab);
+}
+
+stage_status stage_token_probs(stage_dtype dtype, const void* logits, int64_t ld, int32_t rows,
+                               int32_t vocab, const float* temperature, stage_dtype out_dtype,
+                               void* probs, int64_t ld_out, void* ws, size_t ws_bytes,
+                               void* stream) {
+  const int d = (int)dtype, o = (int)out_dtype;
+  if (!is_dtype(d) || !is_dtype(o))
+    return op_fail(STAGE_ERR_UNSUPPORTED, "dtypes %d, %d not supported", d, o);
+  if (rows < 0 || vocab < 1)
+    return op_fail(STAGE_ERR_INVALID_ARG, "%d rows of %d logits", rows, vocab);
+  if (vocab > kMaxVocab) return op_fail(STAGE_ERR_UNSUPPORTED, "vocab %d > %d", vocab, kMaxVocab);
+  if (rows == 0) return STAGE_OK;
+  stage_status v = check_rows(logits, ld, vocab, esize(d), "logits");
+  if (v != STAGE_OK) return v;
+  if ((v = check_rows(probs, ld_out, vocab, esize(o), "probs")) != STAGE_OK) return v;
+  if (probs == logits && (d != o || ld != ld_out))
+    return op_fail(STAGE_ERR_INVALID_ARG, "in place, type and row stride must be the logits'");
+  if (!at_multiple(temperature, 4))
+    return op_fail(STAGE_ERR_INVALID_ARG, "temperature is not aligned to its type");
+  if ((v = check_workspace(ws, ws_bytes, token_probs_bytes(rows, vocab))) != STAGE_OK) return v;
+  return launched("token_probs", token_probs((DType)d, logits, ld, rows, vocab, temperature,
+                                             (DType)o, probs, ld_out, ws, (hipStream_t)stream));
+}
+
+size_t stage_verify_bytes(int32_t num_seqs, int32_t vocab) {
+  return num_seqs < 0 || vocab < 1 || vocab > kMaxVocab ? 0 : verify_bytes(num_seqs, vocab);
+}
+
+stage_status stage_verify_drafts(const stage_drafts* b, int32_t* n_accepted, int32_t* tokens,
+                                 void* ws, size_t ws_bytes, void* stream) {
+  if (!b) return op_fail(STAGE_ERR_INVALID_ARG, "drafts is NULL");
+  const int d = (int)b->dtype;
+  if (!is_dtype(d)) return op_fail(STAGE_ERR_UNSUPPORTED, "dtype %d not supported", d);
+  if (b->num_seqs < 0 || b->num_drafts < 0 || b->max_drafts < 0 || b->vocab < 1)
+    return op_fail(STAGE_ERR_INVALID_ARG, "%d sequences, %d drafts, at most %d each, vocab %d",
+                   b->num_seqs, b->num_drafts, b->max_drafts, b->vocab);
+  if (b->vocab > kMaxVocab)
+    return op_fail(STAGE_ERR_UNSUPPORTED, "vocab %d > %d", b->vocab, kMaxVocab);
+  if (b->num_seqs > kMaxSeqs)
+    return op_fail(STAGE_ERR_CAPACITY, "%d sequences > %d", b->num_seqs, kMaxSeqs);
+  if (b->num_drafts > INT32_MAX - b->num_seqs)
+    return op_fail(STAGE_ERR_CAPACITY, "%d drafts of %d sequences", b->num_drafts, b->num_seqs);
+  if (b->num_seqs == 0) return STAGE_OK;
+  stage_status v = check_rows(b->target_probs, b->ld_target, b->vocab, esize(d), "target_probs");
+  if (v != STAGE_OK) return v;
+  if (b->draft_probs && (v = check_rows(b->draft_probs, b->ld_draft, b->vocab, esize(d),
+                                        "draft_probs")) != STAGE_OK)
+    return v;
+  const struct {
+    const void* p;
+    bool needed;
+    const char* name;
+  } arrays[] = {{b->drafts, b->num_drafts > 0, "drafts"},
+                {b->starts, true, "starts"},
+                {b->accept_u, b->num_drafts > 0, "accept_u"},
+                {b->sample_u, true, "sample_u"},
+                {n_accepted, true, "n_accepted"},
+                {tokens, true, "tokens"}};
+  for (const auto& x : arrays) {
+    if (x.needed && !x.p) return op_fail(STAGE_ERR_INVALID_ARG, "%s is NULL", x.name);
+    if (!at_multiple(x.p, 4))
+      return op_fail(STAGE_ERR_INVALID_ARG, "%s is not aligned to its type", x.name);
+  }
+  if ((v = check_workspace(ws, ws_bytes, verify_bytes(b->num_seqs, b->vocab))) != STAGE_OK)
+    return v;
+  VerifyArgs a;
+  a.target = b->target_probs;
+  a.ld_target = b->ld_target;
+  a.draft = b->draft_probs;
+  a.ld_draft = b->ld_draft;
+  a.vocab = b->vocab;
+  a.drafts = b->drafts;
+  a.starts = b->starts;
+  a.seqs = b->num_seqs;
+  a.n_drafts = b->num_drafts;
+  a.most = b->max_drafts;
+  a.accept_u = b->accept_u;
+  a.sample_u = b->sample_u;
+  a.n_accepted = n_accepted;
+  a.tokens = tokens;
+  return launched("verify_drafts", verify_drafts((DType)d, a, ws, (hipStream_t)stream));
+}
+
+}  // extern "C"

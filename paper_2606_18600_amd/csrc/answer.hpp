@@ -1,0 +1,68 @@
+// Host-side launchers of the answer operators: 8-bit products, token
+// probabilities and draft verification. Like those of kernels.hpp they enqueue
+// on the given stream, return the launch status and allocate nothing.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kernels.hpp"
+
+namespace stage_k {
+
+// An 8-bit matrix: [rows, K] int8 values and one fp32 scale per row, for
+// activations and weights alike. The values are whole operand fragments of
+// v_mfma_i32_16x16x64_i8 (16 rows x 64 k, 1 KB, lane l holding row l % 16, k
+// (l / 16) * 16 .. + 15): fragment (row / 16, k / 64) at index
+// (row / 16) * (kp / 64) + k / 64, so that 16 rows are one contiguous strip.
+// Rows are padded to 16 (undefined values, whose products nobody stores), K to
+// kp, a multiple of 128, with zeros. The scales follow the values.
+inline size_t quant_kp(int K) { return ((size_t)K + 127) / 128 * 128; }
+inline size_t quant_rows16(int rows) { return ((size_t)rows + 15) / 16 * 16; }
+inline size_t quant_scales_at(int rows, int K) { return quant_rows16(rows) * quant_kp(K); }
+inline size_t quant_bytes(int rows, int K) {
+  return quant_scales_at(rows, K) + quant_rows16(rows) * sizeof(float);
+}
+constexpr int kQuantMaxK = 131072;  // 127 * 127 * K stays below 2^31
+
+// dst = the 8-bit matrix of src [rows, K] (fp32 or bf16, row stride ld).
+hipError_t quant_rows(DType dt, const void* src, int64_t ld, int rows, int K, void* dst,
+                      hipStream_t s);
+// ... of int8 values and scales [rows] that the caller has.
+hipError_t quant_pack(const int8_t* src, int64_t ld, const float* scales, int rows, int K,
+                      void* dst, hipStream_t s);
+// ... of RMSNorm(src) * gain in fp32 (K <= 16384, K % 128 == 0); row t is row
+// idx[t] of src (idx: device, or nullptr for row t).
+hipError_t quant_norm_rows(DType dt, const void* src, const int32_t* idx, const void* gain,
+                           float eps, int rows, int K, void* dst, hipStream_t s);
+// out [M, N] (fp32 or bf16, row stride ldo) = a b^T for the 8-bit matrices a
+// [M, K] and b [N, K].
+hipError_t quant_product(const void* a, int M, const void* b, int N, int K, DType out_dt,
+                         void* out, int64_t ldo, hipStream_t s);
+
+// probs[r] = softmax(logits[r] / temperature[r]) (temperature: device [rows],
+// nullptr for 1). ws: token_probs_bytes().
+size_t token_probs_bytes(int rows, int vocab);
+hipError_t token_probs(DType in_dt, const void* logits, int64_t ld_in, int rows, int vocab,
+                       const float* temperature, DType out_dt, void* probs, int64_t ld_out,
+                       void* ws, hipStream_t s);
+
+struct VerifyArgs {
+  const void* target;  // [n_drafts + seqs, vocab]
+  int64_t ld_target;
+  const void* draft;  // [n_drafts, vocab] or nullptr
+  int64_t ld_draft;
+  int vocab;
+  const int32_t* drafts;  // [n_drafts]
+  const int32_t* starts;  // [seqs + 1]
+  int seqs, n_drafts, most;
+  const float* accept_u;  // [n_drafts]
+  const float* sample_u;  // [seqs]
+  int32_t* n_accepted;    // [seqs]
+  int32_t* tokens;        // [seqs, most + 1]
+};
+size_t verify_bytes(int seqs, int vocab);
+hipError_t verify_drafts(DType dt, const VerifyArgs& a, void* ws, hipStream_t s);
+
+}  // namespace stage_k

@@ -1,0 +1,383 @@
+// Products in 8-bit integers: out[m][n] = (sum_k a[m][k] b[n][k]) s_m t_n with
+// int8 values, exact int32 sums (v_mfma_i32_16x16x64_i8) and an fp32 scale per
+// row of either operand. Operands are in the fragment layout of answer.hpp.
+#include <algorithm>
+
+#include "answer.hpp"
+#include "common.hpp"
+
+namespace stage_k {
+
+namespace {
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ i32x4_t mfma_i8(u32x4_t a, u32x4_t b, i32x4_t c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a),
+                                               __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
+}
+
+// Byte offset of the 16 values k = 16 kc .. + 15 of a row; KT = kp / 64.
+__device__ __forceinline__ size_t chunk_offset(int row, int kc, int KT) {
+  return ((size_t)(row >> 4) * KT + (kc >> 2)) * 1024 + ((row & 15) + 16 * (kc & 3)) * 16;
+}
+
+// ---------------------------------------------------------------------------
+// rows -> 8 bits
+// ---------------------------------------------------------------------------
+// s = max(max_k |x_k| / 127, 2^-120), q_k = rint(x_k * (1 / s)): division and
+// products rounded to nearest in fp32, so every implementation of the formula
+// gets the same integers. The floor keeps 1 / s finite for rows of zeros. The
+// maximum is taken over the values' bits, whose order puts NaN above infinity:
+// a row with either gets a scale that is not finite, hence outputs of NaN,
+// and no other row is touched.
+constexpr float kMinScale = 0x1p-120f;
+
+__device__ __forceinline__ float row_scale(uint32_t max_bits) {
+  const float s = __uint_as_float(max_bits) / 127.0f;
+  return s < kMinScale ? kMinScale : s;
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// 16 values of a row from column k, zeros from column K on.
+__device__ __forceinline__ void load16(const float* row, int k, int K, bool whole, float (&v)[16]) {
+  if (whole) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4_t w = *(const f32x4_t*)(row + k + 4 * j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * j + e] = w[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = k + e < K ? row[k + e] : 0.f;
+  }
+}
+__device__ __forceinline__ void load16(const bf16_t* row, int k, int K, bool whole, float (&v)[16]) {
+  if (whole) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const u32x4_t w = ldg128(row + k + 8 * j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[8 * j + 2 * e] = lo_bf16(w[e]);
+        v[8 * j + 2 * e + 1] = hi_bf16(w[e]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = k + e < K ? bf16_to_f32(row[k + e]) : 0.f;
+  }
+}
+
+__device__ __forceinline__ u32x4_t quantise16(const float (&v)[16], float inv) {
+  u32x4_t w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      b |= ((uint32_t)(int)rintf(v[4 * j + e] * inv) & 255u) << (8 * e);
+    w[j] = b;
+  }
+  return w;
+}
+
+// A block takes ROWS rows, 512 / ROWS threads to a row: thread tau row tau %
+// ROWS, 16-value chunks tau / ROWS + (512 / ROWS) c. With 8 rows a store
+// instruction covers whole 128-byte lines of the packed layout (8 rows x 16
+// bytes); one row per block gives few rows their parallelism. The row is read
+// a second time for the rounding, from L2.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(512) void quant_rows_kernel(const T* __restrict__ src, int64_t ld,
+                                                         int rows, int K, int KT, bool aligned,
+                                                         char* __restrict__ dst,
+                                                         float* __restrict__ scales) {
+  constexpr int P = 512 / ROWS;
+  __shared__ uint32_t red[8][ROWS];
+  const int r = threadIdx.x % ROWS, p = threadIdx.x / ROWS;
+  const int row = blockIdx.x * ROWS + r;
+  const bool live = row < rows;
+  const T* x = src + (int64_t)(live ? row : rows - 1) * ld;
+  const int chunks = KT * 4;
+  uint32_t m = 0;
+  for (int c = p; c < chunks; c += P) {
+    float v[16];
+    load16(x, c * 16, K, aligned && c * 16 + 16 <= K, v);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m = max(m, abs_bits(v[e]));
+  }
+#pragma unroll
+  for (int o = 32; o >= ROWS; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  if ((threadIdx.x & 63) < ROWS) red[threadIdx.x >> 6][r] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = max(m, red[w][r]);
+  const float s = row_scale(m), inv = 1.0f / s;
+  if (!live) return;
+  if (p == 0) scales[row] = s;
+  for (int c = p; c < chunks; c += P) {
+    float v[16];
+    load16(x, c * 16, K, aligned && c * 16 + 16 <= K, v);
+    *(u32x4_t*)(dst + chunk_offset(row, c, KT)) = quantise16(v, inv);
+  }
+}
+
+// RMSNorm(x) * gain, then the same: one block per row, the row in registers (K
+// <= 16384: two chunks per thread). The normed values are rounded straight to 8
+// bits, not to the mode dtype first.
+template <typename T>
+__global__ __launch_bounds__(512) void quant_norm_kernel(const T* __restrict__ src,
+                                                         const int32_t* __restrict__ idx,
+                                                         const T* __restrict__ gain, float eps,
+                                                         int K, int KT, char* __restrict__ dst,
+                                                         float* __restrict__ scales) {
+  __shared__ float sum[8];
+  __shared__ uint32_t red[8];
+  const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const T* x = src + (size_t)(idx ? idx[row] : row) * K;
+  const int chunks = K / 16;
+  float v[2][16];
+  float ss = 0.f;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int ch = threadIdx.x + 512 * c;
+    if (ch < chunks) {
+      load16(x, ch * 16, K, true, v[c]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ss += v[c][e] * v[c][e];
+    }
+  }
+  ss = wave_sum(ss);
+  if (lane == 0) sum[wave] = ss;
+  __syncthreads();
+  float tot = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) tot += sum[w];
+  const float rs = 1.0f / sqrtf(tot / (float)K + eps);
+  uint32_t m = 0;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int ch = threadIdx.x + 512 * c;
+    if (ch < chunks) {
+      float g[16];
+      load16(gain, ch * 16, K, true, g);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        v[c][e] = v[c][e] * rs * g[e];
+        m = max(m, abs_bits(v[c][e]));
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  if (lane == 0) red[wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = max(m, red[w]);
+  const float s = row_scale(m), inv = 1.0f / s;
+  if (threadIdx.x == 0) scales[row] = s;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int ch = threadIdx.x + 512 * c;
+    if (ch < chunks) *(u32x4_t*)(dst + chunk_offset(row, ch, KT)) = quantise16(v[c], inv);
+  }
+}
+
+__global__ __launch_bounds__(256) void quant_pack_kernel(const int8_t* __restrict__ src, int64_t ld,
+                                                         const float* __restrict__ s, int rows,
+                                                         int K, int KT, bool aligned,
+                                                         char* __restrict__ dst,
+                                                         float* __restrict__ scales) {
+  const int64_t total = (int64_t)rows * KT * 4, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+    // 8 rows a turn, so that a wave's stores fill lines (as above)
+    const int64_t per = (int64_t)KT * 4 * 8, g = i / per;
+    const int in = (int)min<int64_t>(8, rows - g * 8);  // rows of this turn
+    const int j = (int)(i - g * per);
+    const int row = (int)(g * 8) + j % in, c = j / in;
+    const int8_t* x = src + row * ld;
+    u32x4_t w = {0u, 0u, 0u, 0u};
+    if (aligned && c * 16 + 16 <= K) {
+      w = ldg128(x + c * 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (c * 16 + e < K) w[e / 4] |= (uint32_t)(uint8_t)x[c * 16 + e] << (8 * (e % 4));
+    }
+    *(u32x4_t*)(dst + chunk_offset(row, c, KT)) = w;
+    if (c == 0) scales[row] = s[row];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// few rows: weights streamed once
+// ---------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return f32_to_bf16(v); }
+
+// A block owns NF strips of 16 columns and MT of 16 rows for all of K; its 8
+// waves take k tiles w, w + 8, ... of 64 each, operands straight into registers
+// DEPTH tiles ahead, and add their int32 sums in LDS (integer sums do not depend
+// on their order).
+template <int MT, int NF, int DEPTH, typename OutT>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
+void quant_stream_kernel(const char* __restrict__ A, const float* __restrict__ sa,
+                         const char* __restrict__ B, const float* __restrict__ sb, int M, int N,
+                         int KT, OutT* __restrict__ out, int64_t ldo) {
+  constexpr int NW = 8;
+  __shared__ int red[MT * NF * 256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int strips = (N + 15) / 16;
+  const int n0 = blockIdx.x * NF, m0 = blockIdx.y * MT;
+  const char* bp[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f)
+    bp[f] = B + ((size_t)min(n0 + f, strips - 1) * KT + wave) * 1024 + lane * 16;
+  const char* ap = A + ((size_t)m0 * KT + wave) * 1024 + lane * 16;
+  const int left = M - m0 * 16 - (lane & 15);  // row 16 i of this lane is there if 16 i < left
+  for (int e = threadIdx.x; e < MT * NF * 256; e += 512) red[e] = 0;
+
+  i32x4_t acc[MT][NF];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) acc[i][f] = i32x4_t{0, 0, 0, 0};
+  u32x4_t w[DEPTH][NF], a[DEPTH][MT];
+  const int n = wave < KT ? (KT - wave + NW - 1) / NW : 0;
+  auto load = [&](int d, int t) {
+    t = t < n ? t : n - 1;  // past the end: a valid tile, never used
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      w[d][f] = __builtin_nontemporal_load((const u32x4_t*)(bp[f] + (size_t)t * NW * 1024));
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+      a[d][i] = i * 16 < left ? ldg128(ap + ((size_t)i * KT + (size_t)t * NW) * 1024)
+                              : u32x4_t{0u, 0u, 0u, 0u};
+  };
+  auto compute = [&](int d) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) acc[i][f] = mfma_i8(a[d][i], w[d][f], acc[i][f]);
+  };
+  if (n > 0) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(d, d);
+    int t = 0;
+    for (; t + DEPTH <= n; t += DEPTH) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        __builtin_amdgcn_sched_barrier(0);
+        compute(d);
+        __builtin_amdgcn_sched_barrier(0);
+        load(d, t + DEPTH + d);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d)
+      if (t + d < n) compute(d);
+  }
+  __syncthreads();
+  if (n > 0) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          atomicAdd(&red[((i * NF + f) * 4 + r) * 64 + lane], acc[i][f][r]);
+  }
+  __syncthreads();
+  // value r of lane l of a tile: row (l / 16) * 4 + r, column l % 16
+  for (int e = threadIdx.x; e < MT * NF * 256; e += 512) {
+    const int c = e % (NF * 16), mr = e / (NF * 16);
+    const int m = m0 * 16 + mr, col = n0 * 16 + c;
+    if (m >= M || col >= N) continue;
+    const int i = mr >> 4, f = c >> 4;
+    const int v = red[((i * NF + f) * 4 + (mr & 3)) * 64 + ((mr >> 2) & 3) * 16 + (c & 15)];
+    out[(int64_t)m * ldo + col] = from_f32<OutT>((float)v * (sa[m] * sb[col]));
+  }
+}
+
+template <typename OutT>
+hipError_t launch_product(const char* a, const float* sa, const char* b, const float* sb, int M,
+                          int N, int KT, OutT* out, int64_t ldo, hipStream_t s) {
+  const int strips = (N + 15) / 16, tiles = (M + 15) / 16;
+  const dim3 grid((strips + 1) / 2, (tiles + 3) / 4);
+  if (tiles == 1)
+    quant_stream_kernel<1, 2, 4, OutT><<<grid, 512, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
+  else
+    quant_stream_kernel<4, 2, 2, OutT><<<grid, 512, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
+  return hipGetLastError();
+}
+
+bool aligned16(const void* p, int64_t row_bytes) {
+  return ((uintptr_t)p | (uintptr_t)row_bytes) % 16 == 0;
+}
+
+template <typename T>
+hipError_t launch_quant_rows(const T* src, int64_t ld, int rows, int K, char* dst, float* scales,
+                             hipStream_t s) {
+  const int KT = (int)(quant_kp(K) / 64);
+  const bool al = aligned16(src, ld * (int64_t)sizeof(T));
+  if (rows >= 1024)
+    quant_rows_kernel<T, 8><<<(rows + 7) / 8, 512, 0, s>>>(src, ld, rows, K, KT, al, dst, scales);
+  else
+    quant_rows_kernel<T, 1><<<rows, 512, 0, s>>>(src, ld, rows, K, KT, al, dst, scales);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t quant_rows(DType dt, const void* src, int64_t ld, int rows, int K, void* dst,
+                      hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  char* d = (char*)dst;
+  float* scales = (float*)(d + quant_scales_at(rows, K));
+  if (dt == DT_F32)
+    return launch_quant_rows((const float*)src, ld, rows, K, d, scales, s);
+  return launch_quant_rows((const bf16_t*)src, ld, rows, K, d, scales, s);
+}
+
+hipError_t quant_pack(const int8_t* src, int64_t ld, const float* scales, int rows, int K,
+                      void* dst, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  const int KT = (int)(quant_kp(K) / 64);
+  const int64_t blocks = ((int64_t)rows * KT * 4 + 255) / 256;
+  quant_pack_kernel<<<(int)std::min<int64_t>(blocks, 16384), 256, 0, s>>>(
+      src, ld, scales, rows, K, KT, aligned16(src, ld), (char*)dst,
+      (float*)((char*)dst + quant_scales_at(rows, K)));
+  return hipGetLastError();
+}
+
+hipError_t quant_norm_rows(DType dt, const void* src, const int32_t* idx, const void* gain,
+                           float eps, int rows, int K, void* dst, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  if (K > 16384 || K % 128 != 0) return hipErrorInvalidValue;
+  char* d = (char*)dst;
+  float* scales = (float*)(d + quant_scales_at(rows, K));
+  if (dt == DT_F32)
+    quant_norm_kernel<float><<<rows, 512, 0, s>>>((const float*)src, idx, (const float*)gain, eps,
+                                                  K, K / 64, d, scales);
+  else
+    quant_norm_kernel<bf16_t><<<rows, 512, 0, s>>>((const bf16_t*)src, idx, (const bf16_t*)gain,
+                                                   eps, K, K / 64, d, scales);
+  return hipGetLastError();
+}
+
+hipError_t quant_product(const void* a, int M, const void* b, int N, int K, DType out_dt,
+                         void* out, int64_t ldo, hipStream_t s) {
+  if (M == 0) return hipSuccess;
+  const char *ac = (const char*)a, *bc = (const char*)b;
+  const float* sa = (const float*)(ac + quant_scales_at(M, K));
+  const float* sb = (const float*)(bc + quant_scales_at(N, K));
+  const int KT = (int)(quant_kp(K) / 64);
+  if (out_dt == DT_F32)
+    return launch_product(ac, sa, bc, sb, M, N, KT, (float*)out, ldo, s);
+  return launch_product(ac, sa, bc, sb, M, N, KT, (bf16_t*)out, ldo, s);
+}
+
+}  // namespace stage_k

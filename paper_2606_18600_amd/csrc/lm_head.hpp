@@ -1,0 +1,40 @@
+// The LM head's call, shared by its products: argument checks, the selected
+// rows, the stage's workspace and op timing are the same whatever the type of
+// the weights.
+#pragma once
+
+#include "../../include/stage.h"
+#include "kernels.hpp"
+
+namespace stage_k {
+
+// What a call's kernels read: row t is hidden row idx[t] (idx: device, or
+// nullptr for row t). x and h are the workspace's fp32 rows and activations.
+struct LmHeadRows {
+  DType dt = DT_F32;
+  const void* hidden = nullptr;
+  const int32_t* idx = nullptr;
+  const void* gain = nullptr;
+  int n = 0, H = 0;
+  float eps = 0.f;
+  float* x = nullptr;
+  void* h = nullptr;
+  size_t h_bytes = 0;
+  int skinny_rows = 0;
+};
+
+// The two launches of a call: the normed rows into r.h, and their product with
+// w [vocab, H].
+struct LmHeadProduct {
+  hipError_t (*norm)(const LmHeadProduct&, const LmHeadRows&, hipStream_t) = nullptr;
+  hipError_t (*product)(const LmHeadProduct&, const LmHeadRows&, hipStream_t) = nullptr;
+  const void* w = nullptr;
+  int vocab = 0, vocab_multiple = 1;
+  float* logits = nullptr;
+};
+
+stage_status lm_head_rows(stage_t* st, const LmHeadProduct& f, const void* final_norm,
+                          const void* hidden, int32_t hidden_rows, const int32_t* rows,
+                          int32_t n_rows, void* stream);
+
+}  // namespace stage_k

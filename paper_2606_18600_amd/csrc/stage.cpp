@@ -17,6 +17,7 @@
 
 #include "../../include/stage.h"
 #include "kernels.hpp"
+#include "lm_head.hpp"
 
 using namespace stage_k;
 
@@ -797,6 +798,59 @@ stage_status run_step(stage* st, const stage_batch* pf, const stage_batch* dc, c
 
 }  // namespace
 
+stage_status stage_k::lm_head_rows(stage* st, const LmHeadProduct& f, const void* final_norm,
+                                   const void* hidden, int32_t hidden_rows, const int32_t* rows,
+                                   int32_t n_rows, void* stream) {
+  if (!st) return fail(STAGE_ERR_INVALID_ARG, "stage is NULL");
+  if (!st->ws) return fail(STAGE_ERR_INVALID_ARG, "no workspace bound (stage_bind_workspace)");
+  if (!final_norm || !f.w || !hidden || (!f.logits && n_rows != 0))
+    return fail(STAGE_ERR_INVALID_ARG, "final_norm/w_lm/hidden/logits is NULL");
+  const auto& c = st->cfg;
+  if (f.vocab <= 0 || hidden_rows < 0 || n_rows < 0)
+    return fail(STAGE_ERR_INVALID_ARG, "vocab must be positive, row counts >= 0");
+  if (f.vocab % f.vocab_multiple != 0)
+    return fail(STAGE_ERR_UNSUPPORTED, "vocab %d is not a multiple of %d", f.vocab,
+                f.vocab_multiple);
+  if (n_rows == 0) return STAGE_OK;
+  if (n_rows > st->max_tokens)
+    return fail(STAGE_ERR_CAPACITY, "%d rows > max_tokens %d", n_rows, st->max_tokens);
+  if (rows) {
+    for (int i = 0; i < n_rows; ++i)
+      if (rows[i] < 0 || rows[i] >= hidden_rows)
+        return fail(STAGE_ERR_INVALID_ARG, "rows[%d] = %d outside [0, %d)", i, rows[i],
+                    hidden_rows);
+  } else if (n_rows > hidden_rows) {
+    return fail(STAGE_ERR_INVALID_ARG, "%d rows > hidden_rows %d", n_rows, hidden_rows);
+  }
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e = hipSetDevice(st->device);
+  if (e != hipSuccess) return hip_fail("hipSetDevice", e);
+  LmHeadRows r;
+  if (rows) {
+    int slot = 0;
+    stage_status vs = take_slot(st, &slot);
+    if (vs != STAGE_OK) return vs;
+    std::memcpy(st->staging[slot], rows, (size_t)n_rows * 4);
+    if ((vs = upload_slot(st, slot, n_rows, s)) != STAGE_OK) return vs;
+    r.idx = st->at<int32_t>(st->r_meta);
+  }
+  r.dt = (DType)c.dtype;
+  r.hidden = hidden;
+  r.gain = final_norm;
+  r.n = n_rows;
+  r.H = c.hidden;
+  r.eps = c.rms_eps;
+  r.x = st->at<float>(st->r_x);
+  r.h = st->ws + st->r_h.off;
+  r.h_bytes = st->r_h.bytes;
+  r.skinny_rows = st->skinny_rows;
+  Launcher L{st, s};
+  L(STAGE_OP_LM_HEAD, [&] { return f.norm(f, r, s); });
+  L(STAGE_OP_LM_HEAD, [&] { return f.product(f, r, s); });
+  if (L.err != hipSuccess) return hip_fail("kernel launch", L.err);
+  return STAGE_OK;
+}
+
 extern "C" {
 
 stage_status stage_create(const stage_model_config* cfg, int32_t layer_begin, int32_t layer_end,
@@ -1037,51 +1091,20 @@ stage_status stage_lm_head(stage_t* st, const void* final_norm, const void* w_lm
                            const void* hidden, int32_t hidden_rows, const int32_t* rows,
                            int32_t n_rows, float* logits, void* stream) {
   if (!st) return fail(STAGE_ERR_INVALID_ARG, "stage is NULL");
-  if (!st->ws) return fail(STAGE_ERR_INVALID_ARG, "no workspace bound (stage_bind_workspace)");
-  if (!final_norm || !w_lm || !hidden || !logits)
-    return fail(STAGE_ERR_INVALID_ARG, "final_norm/w_lm/hidden/logits is NULL");
-  const auto& c = st->cfg;
-  if (vocab <= 0 || hidden_rows < 0 || n_rows < 0)
-    return fail(STAGE_ERR_INVALID_ARG, "vocab must be positive, row counts >= 0");
-  if (c.dtype == STAGE_BF16 && vocab % 128 != 0)
-    return fail(STAGE_ERR_UNSUPPORTED, "vocab %d is not a multiple of 128", vocab);
-  if (n_rows == 0) return STAGE_OK;
-  if (n_rows > st->max_tokens)
-    return fail(STAGE_ERR_CAPACITY, "%d rows > max_tokens %d", n_rows, st->max_tokens);
-  if (rows) {
-    for (int i = 0; i < n_rows; ++i)
-      if (rows[i] < 0 || rows[i] >= hidden_rows)
-        return fail(STAGE_ERR_INVALID_ARG, "rows[%d] = %d outside [0, %d)", i, rows[i],
-                    hidden_rows);
-  } else if (n_rows > hidden_rows) {
-    return fail(STAGE_ERR_INVALID_ARG, "%d rows > hidden_rows %d", n_rows, hidden_rows);
-  }
-  hipStream_t s = (hipStream_t)stream;
-  hipError_t e = hipSetDevice(st->device);
-  if (e != hipSuccess) return hip_fail("hipSetDevice", e);
-  const int32_t* rows_dev = nullptr;
-  if (rows) {
-    int slot = 0;
-    stage_status vs = take_slot(st, &slot);
-    if (vs != STAGE_OK) return vs;
-    std::memcpy(st->staging[slot], rows, (size_t)n_rows * 4);
-    if ((vs = upload_slot(st, slot, n_rows, s)) != STAGE_OK) return vs;
-    rows_dev = st->at<int32_t>(st->r_meta);
-  }
-  const DType dt = (DType)c.dtype;
-  const int H = c.hidden;
-  float* x = st->at<float>(st->r_x);
-  void* h = st->ws + st->r_h.off;
-  Launcher L{st, s};
-  L(STAGE_OP_LM_HEAD, [&] {
-    return embed_norm(dt, hidden, x, h, final_norm, n_rows, H, c.rms_eps, s, rows_dev);
-  });
-  if (dt == DT_BF16 && n_rows <= st->skinny_rows)
-    L(STAGE_OP_LM_HEAD, [&] { return gemm_skinny(h, w_lm, n_rows, vocab, H, 1, false, logits, s); });
-  else
-    L(STAGE_OP_LM_HEAD, [&] { return gemm(dt, EPI_STORE_F32, h, w_lm, n_rows, vocab, H, logits, s); });
-  if (L.err != hipSuccess) return hip_fail("kernel launch", L.err);
-  return STAGE_OK;
+  LmHeadProduct f;
+  f.norm = [](const LmHeadProduct&, const LmHeadRows& r, hipStream_t s) {
+    return embed_norm(r.dt, r.hidden, r.x, r.h, r.gain, r.n, r.H, r.eps, s, r.idx);
+  };
+  f.product = [](const LmHeadProduct& p, const LmHeadRows& r, hipStream_t s) {
+    if (r.dt == DT_BF16 && r.n <= r.skinny_rows)
+      return gemm_skinny(r.h, p.w, r.n, p.vocab, r.H, 1, false, p.logits, s);
+    return gemm(r.dt, EPI_STORE_F32, r.h, p.w, r.n, p.vocab, r.H, p.logits, s);
+  };
+  f.w = w_lm;
+  f.vocab = vocab;
+  f.vocab_multiple = st->cfg.dtype == STAGE_BF16 ? 128 : 1;
+  f.logits = logits;
+  return lm_head_rows(st, f, final_norm, hidden, hidden_rows, rows, n_rows, stream);
 }
 
 stage_status stage_destroy(stage_t* st) {

@@ -8,11 +8,12 @@ tensors, creates the stage over them and forwards calls.
 
 from __future__ import annotations
 
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, Optional, Sequence, Union
 
 import numpy as np
 import torch
 
+from . import int8
 from . import stage as S
 from .synth import GAIN_NAMES, ModelShape, _TENSOR_IDS
 
@@ -172,16 +173,23 @@ class DeviceStage:
         S.stage_step_mixed(self.handle, pb, db, hidden_in.data_ptr(), out.data_ptr(), stream)
         return out
 
-    def lm_head(self, final_norm: torch.Tensor, w_lm_packed: torch.Tensor, hidden: torch.Tensor,
-                rows=None, n_rows: Optional[int] = None, logits: Optional[torch.Tensor] = None,
-                stream=0) -> torch.Tensor:
-        """Logits [n_rows, vocab] (fp32) of the selected rows of `hidden`."""
+    def lm_head(self, final_norm: torch.Tensor, w_lm_packed: Union[torch.Tensor, int8.Matrix],
+                hidden: torch.Tensor, rows=None, n_rows: Optional[int] = None,
+                logits: Optional[torch.Tensor] = None, stream=0) -> torch.Tensor:
+        """Logits [n_rows, vocab] (fp32) of the selected rows of `hidden`, over
+        a packed LM head or one quantised to 8 bits."""
         vocab = w_lm_packed.shape[0]
         n = len(rows) if rows is not None else (hidden.shape[0] if n_rows is None else n_rows)
         if logits is None:
             logits = torch.empty((n, vocab), dtype=torch.float32, device=hidden.device)
-        S.stage_lm_head(self.handle, final_norm.data_ptr(), w_lm_packed.data_ptr(), vocab,
-                        hidden.data_ptr(), hidden.shape[0], rows, n, logits.data_ptr(), stream)
+        if isinstance(w_lm_packed, int8.Matrix):
+            if w_lm_packed.k != self.shape.hidden:
+                raise int8.invalid(f"LM head {w_lm_packed.shape} for hidden {self.shape.hidden}")
+            call, w = S.stage_lm_head_quant, w_lm_packed.data
+        else:
+            call, w = S.stage_lm_head, w_lm_packed
+        call(self.handle, final_norm.data_ptr(), w.data_ptr(), vocab, hidden.data_ptr(),
+             hidden.shape[0], rows, n, logits.data_ptr(), stream)
         return logits
 
     def kv_view(self) -> torch.Tensor:

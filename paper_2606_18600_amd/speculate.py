@@ -1,0 +1,112 @@
+"""From logits to tokens over torch tensors (``stage_token_probs`` and
+``stage_verify_drafts`` of the ABI): what the last stage of a pipeline does after
+its LM head when a draft model, or a table, proposes several tokens per request and
+step::
+
+    logits = st.lm_head(final_norm, w_lm, hidden, rows)     # n_i + 1 rows a request
+    probs = speculate.token_probs(logits, temperature)
+    n, tokens = speculate.verify_drafts(probs, draft_probs, drafts, starts, most,
+                                        accept_u, sample_u)
+
+Random numbers are arguments: the same ones give the same tokens. Everything runs
+on torch's current stream of the tensors' device; outputs and scratch come from
+torch's allocator, so calls may be captured into a graph.
+"""
+
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import stage as S
+from .int8 import DTYPES, at_device, invalid, on_gpu, row_stride, rows_of, unsupported
+
+
+def token_probs(logits: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                dtype: torch.dtype = torch.float32,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """softmax(logits / temperature) over the last dimension. logits [..., vocab]
+    fp32 or bf16; temperature fp32, one per row (None: 1; 0: the largest logit,
+    the lowest token among equals). The result is in ``dtype``, or in ``out``
+    ([rows, vocab], any row stride), which may be the logits themselves."""
+    dt = DTYPES.get(logits.dtype)
+    dt_out = DTYPES.get(dtype if out is None else out.dtype)
+    if dt is None or dt_out is None:
+        raise unsupported(f"token_probs: {logits.dtype} to {dtype if out is None else out.dtype}")
+    device = on_gpu(logits, temperature, out)
+    shape = logits.shape
+    logits = rows_of(logits, "logits")
+    rows, vocab = logits.shape
+    if temperature is not None:
+        if temperature.dtype != torch.float32 or temperature.numel() != rows:
+            raise invalid(f"temperature must be float32, one for each of {rows} rows")
+        temperature = temperature.reshape(-1).contiguous()
+    if out is not None and (out.shape != (rows, vocab) or (vocab > 1 and out.stride(1) != 1) or
+                            (rows > 1 and out.stride(0) < vocab)):
+        raise invalid(f"out {tuple(out.shape)} with strides {out.stride()}")
+    with at_device(device) as stream:
+        if out is None:
+            out = torch.empty((rows, vocab), dtype=dtype, device=device)
+            result = out if len(shape) == 2 else out.view(shape)
+        else:
+            result = out
+        size = S.stage_token_probs_bytes(rows, vocab)
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        S.stage_token_probs(dt, logits.data_ptr(), row_stride(logits), rows, vocab,
+                            None if temperature is None else temperature.data_ptr(), dt_out,
+                            out.data_ptr(), row_stride(out), ws.data_ptr(), size, stream)
+    return result
+
+
+def _array(t: torch.Tensor, n: int, dtype: torch.dtype, what: str) -> torch.Tensor:
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
+        raise invalid(f"{what} must be {dtype} [{n}], not {t.dtype} {tuple(t.shape)}")
+    return t.contiguous()
+
+
+def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor],
+                  drafts: torch.Tensor, starts: torch.Tensor, max_drafts: int,
+                  accept_u: torch.Tensor, sample_u: torch.Tensor
+                  ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Accepted drafts per sequence [num_seqs] and its new tokens [num_seqs,
+    max_drafts + 1] (the accepted drafts, the drawn token, -1 after it), int32.
+
+    Sequence i has the drafts starts[i] .. starts[i + 1] - 1 (at most max_drafts);
+    target_probs [num_drafts + num_seqs, vocab] holds its rows one after another, one
+    for each draft and one for the token after the last; draft_probs [num_drafts,
+    vocab] what each draft was drawn from (None: chosen outright). Probabilities
+    fp32 or bf16, drafts and starts int32, the random numbers fp32."""
+    dt = DTYPES.get(target_probs.dtype)
+    if dt is None:
+        raise unsupported(f"verify_drafts: {target_probs.dtype}")
+    if target_probs.dim() != 2 or drafts.dim() != 1 or starts.dim() != 1 or starts.shape[0] < 1:
+        raise invalid("verify_drafts: target_probs must be [rows, vocab], drafts and starts lists")
+    device = on_gpu(target_probs, draft_probs, drafts, starts, accept_u, sample_u)
+    n, seqs, vocab = drafts.shape[0], starts.shape[0] - 1, target_probs.shape[1]
+    if target_probs.shape[0] != n + seqs:
+        raise invalid(f"{target_probs.shape[0]} target rows for {n} drafts of {seqs} sequences")
+    if draft_probs is not None and (draft_probs.dtype != target_probs.dtype or
+                                    draft_probs.shape != (n, vocab)):
+        raise invalid(f"draft_probs must be {target_probs.dtype} [{n}, {vocab}]")
+    p = rows_of(target_probs, "target_probs")
+    q = None if draft_probs is None else rows_of(draft_probs, "draft_probs")
+    drafts = _array(drafts, n, torch.int32, "drafts")
+    starts = _array(starts, seqs + 1, torch.int32, "starts")
+    accept_u = _array(accept_u, n, torch.float32, "accept_u")
+    sample_u = _array(sample_u, seqs, torch.float32, "sample_u")
+    if max_drafts < 0:
+        raise invalid(f"max_drafts {max_drafts}")
+    with at_device(device) as stream:
+        n_accepted = torch.empty(seqs, dtype=torch.int32, device=device)
+        tokens = torch.empty((seqs, max_drafts + 1), dtype=torch.int32, device=device)
+        size = S.stage_verify_bytes(seqs, vocab)
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+        # an empty draft_probs stays "given": no draft is there to ask
+        batch = S.stage_drafts(dt, vocab, seqs, n, max_drafts, p.data_ptr(), row_stride(p),
+                               None if q is None or n == 0 else q.data_ptr(),
+                               0 if q is None else row_stride(q), drafts.data_ptr(),
+                               starts.data_ptr(), accept_u.data_ptr(), sample_u.data_ptr())
+        S.stage_verify_drafts(batch, n_accepted.data_ptr(), tokens.data_ptr(), ws.data_ptr(), size,
+                              stream)
+    return n_accepted, tokens

@@ -37,7 +37,10 @@ EXPORTED = ("stage_create", "stage_workspace_bytes", "stage_bind_workspace", "st
             "stage_validate_step", "stage_set_op_timing", "stage_read_op_times",
             "stage_pack_weight", "stage_copy_probe", "stage_lm_head", "stage_pack_lm_head",
             "stage_decode_noalloc", "stage_store_alloc", "stage_store_free", "stage_store_write",
-            "stage_store_attach", "stage_store_detach")
+            "stage_store_attach", "stage_store_detach", "stage_quant_bytes", "stage_quant_rows",
+            "stage_quant_pack", "stage_quant_product", "stage_lm_head_quant",
+            "stage_token_probs_bytes", "stage_token_probs", "stage_verify_bytes",
+            "stage_verify_drafts")
 
 STAGE_STORE_MAX_BYTES = 1 << 31
 
@@ -79,6 +82,16 @@ class stage_batch(ctypes.Structure):
                 ("block_tables", ctypes.c_void_p), ("max_blocks_per_seq", ctypes.c_int32)]
 
 
+class stage_drafts(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("num_seqs", ctypes.c_int32), ("num_drafts", ctypes.c_int32),
+                ("max_drafts", ctypes.c_int32), ("target_probs", ctypes.c_void_p),
+                ("ld_target", ctypes.c_int64), ("draft_probs", ctypes.c_void_p),
+                ("ld_draft", ctypes.c_int64), ("drafts", ctypes.c_void_p),
+                ("starts", ctypes.c_void_p), ("accept_u", ctypes.c_void_p),
+                ("sample_u", ctypes.c_void_p)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -118,6 +131,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.stage_store_write.argtypes = [P, P, ctypes.c_size_t, P]
     lib.stage_store_attach.argtypes = [ctypes.POINTER(stage_ipc_handle), ctypes.POINTER(P)]
     lib.stage_store_detach.argtypes = [P]
+    i64, size = ctypes.c_int64, ctypes.c_size_t
+    lib.stage_quant_bytes.argtypes = [i32, i32]
+    lib.stage_quant_rows.argtypes = [i32, P, i64, i32, i32, P, P]
+    lib.stage_quant_pack.argtypes = [P, i64, P, i32, i32, P, P]
+    lib.stage_quant_product.argtypes = [P, i32, P, i32, i32, i32, P, i64, P]
+    lib.stage_lm_head_quant.argtypes = lib.stage_lm_head.argtypes
+    lib.stage_token_probs_bytes.argtypes = [i32, i32]
+    lib.stage_token_probs.argtypes = [i32, P, i64, i32, i32, P, i32, P, i64, P, size, P]
+    lib.stage_verify_bytes.argtypes = [i32, i32]
+    lib.stage_verify_drafts.argtypes = [ctypes.POINTER(stage_drafts), P, P, P, size, P]
+    for name in ("stage_quant_bytes", "stage_token_probs_bytes", "stage_verify_bytes"):
+        getattr(lib, name).restype = size
     lib.stage_set_op_timing.argtypes = [P, i32]
     lib.stage_read_op_times.argtypes = [P, ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(ctypes.c_int64)]
@@ -127,7 +152,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                  "stage_set_op_timing", "stage_read_op_times", "stage_pack_weight",
                  "stage_copy_probe", "stage_lm_head", "stage_pack_lm_head", "stage_store_alloc",
                  "stage_store_free", "stage_store_write", "stage_store_attach",
-                 "stage_store_detach"):
+                 "stage_store_detach", "stage_quant_rows", "stage_quant_pack",
+                 "stage_quant_product", "stage_lm_head_quant", "stage_token_probs",
+                 "stage_verify_drafts"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -219,18 +246,68 @@ def stage_copy_probe(src: int, dst: int, nbytes: int, stream: int = 0) -> None:
     _check(load_library().stage_copy_probe(src, dst, nbytes, stream))
 
 
+def _row_indices(rows, n_rows: int):
+    if rows is None:
+        return None
+    r = np.ascontiguousarray(rows, dtype=np.int32)
+    if len(r) != n_rows:
+        raise StageError(STAGE_ERR_INVALID_ARG, f"{len(r)} row indices for n_rows={n_rows}")
+    return r.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+
 def stage_lm_head(st: int, final_norm: int, w_lm: int, vocab: int, hidden: int,
                   hidden_rows: int, rows, n_rows: int, logits: int, stream: int = 0) -> None:
     """``rows``: host int32 indices into ``hidden`` (or None for 0..n_rows-1)."""
-    if rows is None:
-        rp = None
-    else:
-        r = np.ascontiguousarray(rows, dtype=np.int32)
-        if len(r) != n_rows:
-            raise StageError(STAGE_ERR_INVALID_ARG, f"{len(r)} row indices for n_rows={n_rows}")
-        rp = r.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
-    _check(load_library().stage_lm_head(st, final_norm, w_lm, vocab, hidden, hidden_rows, rp,
-                                        n_rows, logits, stream))
+    _check(load_library().stage_lm_head(st, final_norm, w_lm, vocab, hidden, hidden_rows,
+                                        _row_indices(rows, n_rows), n_rows, logits, stream))
+
+
+def stage_lm_head_quant(st: int, final_norm: int, w_lm: int, vocab: int, hidden: int,
+                        hidden_rows: int, rows, n_rows: int, logits: int,
+                        stream: int = 0) -> None:
+    """``stage_lm_head`` over a quantised [vocab, hidden] matrix."""
+    _check(load_library().stage_lm_head_quant(st, final_norm, w_lm, vocab, hidden, hidden_rows,
+                                              _row_indices(rows, n_rows), n_rows, logits, stream))
+
+
+def stage_quant_bytes(rows: int, k: int) -> int:
+    return load_library().stage_quant_bytes(rows, k)
+
+
+def stage_quant_rows(dtype: int, src: int, ld: int, rows: int, k: int, dst: int,
+                     stream: int = 0) -> None:
+    _check(load_library().stage_quant_rows(dtype, src, ld, rows, k, dst, stream))
+
+
+def stage_quant_pack(src: int, ld: int, scales: int, rows: int, k: int, dst: int,
+                     stream: int = 0) -> None:
+    _check(load_library().stage_quant_pack(src, ld, scales, rows, k, dst, stream))
+
+
+def stage_quant_product(a: int, m: int, b: int, n: int, k: int, out_dtype: int, out: int,
+                        ldo: int, stream: int = 0) -> None:
+    _check(load_library().stage_quant_product(a, m, b, n, k, out_dtype, out, ldo, stream))
+
+
+def stage_token_probs_bytes(rows: int, vocab: int) -> int:
+    return load_library().stage_token_probs_bytes(rows, vocab)
+
+
+def stage_token_probs(dtype: int, logits: int, ld: int, rows: int, vocab: int,
+                      temperature: Optional[int], out_dtype: int, probs: int, ld_out: int, ws: int,
+                      ws_bytes: int, stream: int = 0) -> None:
+    _check(load_library().stage_token_probs(dtype, logits, ld, rows, vocab, temperature,
+                                            out_dtype, probs, ld_out, ws, ws_bytes, stream))
+
+
+def stage_verify_bytes(num_seqs: int, vocab: int) -> int:
+    return load_library().stage_verify_bytes(num_seqs, vocab)
+
+
+def stage_verify_drafts(batch: stage_drafts, n_accepted: int, tokens: int, ws: int,
+                        ws_bytes: int, stream: int = 0) -> None:
+    _check(load_library().stage_verify_drafts(ctypes.byref(batch), n_accepted, tokens, ws,
+                                              ws_bytes, stream))
 
 
 def stage_pack_lm_head(cfg: stage_model_config, vocab: int, src: int, dst: int,
