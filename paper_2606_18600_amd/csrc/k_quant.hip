@@ -218,6 +218,15 @@ template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return f32_to_bf16(v); }
 
+// 4 adjacent values, at any address that the type allows.
+typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void store4(float* o, const float (&v)[4]) {
+  *(f32x4_any_t*)o = f32x4_any_t{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store4(bf16_t* o, const float (&v)[4]) {
+  *(u32x2_any_t*)o = u32x2_any_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
 // A block owns NF strips of 16 columns and MT of 16 rows for all of K; its 8
 // waves take k tiles w, w + 8, ... of 64 each, operands straight into registers
 // DEPTH tiles ahead, and add their int32 sums in LDS (integer sums do not depend
@@ -302,10 +311,171 @@ void quant_stream_kernel(const char* __restrict__ A, const float* __restrict__ s
   }
 }
 
+// ---------------------------------------------------------------------------
+// many rows: tiles through LDS
+// ---------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+// s_waitcnt immediate: at most n vector-memory operations outstanding (the
+// other counters are not waited for).
+constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+
+// Block tile of BM x BN strips (16 rows, 16 columns each) on WM x WN waves of
+// TM x TN. A stage is one k tile of 64: BM + BN fragments of 1 KB, copied straight
+// into a ring of R slots, R - 1 stages ahead. A wave multiplies in halves of its
+// columns; while it does, half of the next stage's rows and the other half's (the
+// next stage's) columns come out of LDS, six fragments a half on 8 x 4 strips, so
+// that LDS is read evenly. One barrier a stage publishes the copies of stage kt +
+// 1 and frees the slot of stage kt - 1.
+//
+// Bound: power. 2048 x 57344 x 8192 takes 735 us (2.62 Pop/s; a library int8
+// product reaches 2.16 there) at 1.84 GHz with the matrix units busy two thirds of
+// the time; with operands of zeros, hence little switching, 587 us. Measured
+// against it: 4 x 2 waves 750 us, reads in bursts 741, v_mfma_i32_32x32x32_i8 894,
+// four waves of 128 x 128 827, a ring of 5 759.
+template <int BM, int BN, int WM, int WN, int R, typename OutT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
+    const char* __restrict__ A, const float* __restrict__ sa, const char* __restrict__ B,
+    const float* __restrict__ sb, int M, int N, int KT, OutT* __restrict__ out, int64_t ldo) {
+  constexpr int NW = WM * WN, FR = BM + BN, PW = FR / NW, TM = BM / WM, TN = BN / WN, TH = TN / 2;
+  static_assert(FR % NW == 0 && BM % WM == 0 && BN % WN == 0 && TN % 2 == 0, "tile split");
+  __shared__ u32x4_t lds[R][FR * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  // Blocks go round-robin to the 8 XCDs, each with an L2 of its own: give an XCD
+  // whole columns of tiles, so that a weight strip is fetched into one L2.
+  int mb, nb;
+  {
+    const int MB = gridDim.x, NB8 = (int)gridDim.y / 8 * 8;
+    const int lin = blockIdx.x + blockIdx.y * MB;
+    if (lin < MB * NB8) {
+      const int j = lin / 8;
+      nb = (j / MB) * 8 + lin % 8;
+      mb = j % MB;
+    } else {
+      const int rem = lin - MB * NB8;
+      nb = NB8 + rem / MB;
+      mb = rem % MB;
+    }
+  }
+  const int ms = (M + 15) / 16, ns = (N + 15) / 16;
+  const int m0 = mb * BM, n0 = nb * BN;
+  // fragment f of a stage: strip m0 + f of A, then strip n0 + f - BM of B (strips
+  // past the end repeat the last one; nothing of theirs is stored)
+  const char* src[PW];
+#pragma unroll
+  for (int p = 0; p < PW; ++p) {
+    const int f = wave * PW + p;
+    const size_t strip = f < BM ? min(m0 + f, ms - 1) : min(n0 + f - BM, ns - 1);
+    src[p] = (f < BM ? A : B) + strip * KT * 1024;
+  }
+  auto issue = [&](int kt) {
+    const int slot = kt % R;
+    kt = kt < KT ? kt : KT - 1;  // past the end: into a slot that nobody reads
+#pragma unroll
+    for (int p = 0; p < PW; ++p)
+      __builtin_amdgcn_global_load_lds((const void*)(src[p] + (size_t)kt * 1024 + lane * 16),
+                                       (lds_ptr_t)&lds[slot][(wave * PW + p) * 64], 16, 0, 0);
+  };
+  i32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = i32x4_t{0, 0, 0, 0};
+
+  constexpr int AH = TM / 2;
+  auto read_a = [&](u32x4_t (&a)[TM], int slot, int h) {
+#pragma unroll
+    for (int i = h * AH; i < (h + 1) * AH; ++i) a[i] = lds[slot][(wm * TM + i) * 64 + lane];
+  };
+  auto read_b = [&](u32x4_t (&b)[TH], int slot, int h) {
+#pragma unroll
+    for (int j = 0; j < TH; ++j) b[j] = lds[slot][(BM + wn * TN + h * TH + j) * 64 + lane];
+  };
+  auto multiply = [&](const u32x4_t (&a)[TM], const u32x4_t (&b)[TH], int h) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TH; ++j) acc[i][h * TH + j] = mfma_i8(b[j], a[i], acc[i][h * TH + j]);
+  };
+  u32x4_t a0[TM], a1[TM], b0[TH], b1[TH], bh[TH];
+  auto stage = [&](int kt, u32x4_t (&a)[TM], u32x4_t (&b)[TH], u32x4_t (&an)[TM],
+                   u32x4_t (&bn)[TH]) {
+    // this wave's copies of stage kt + 1 have landed; after the barrier all have
+    __builtin_amdgcn_s_waitcnt(vmcnt_at_most((R - 3) * PW));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    issue(kt + R - 1);
+    __builtin_amdgcn_sched_barrier(0);
+    read_b(bh, kt % R, 1);
+    read_a(an, (kt + 1) % R, 0);
+    multiply(a, b, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    read_a(an, (kt + 1) % R, 1);
+    read_b(bn, (kt + 1) % R, 0);
+    multiply(a, bh, 1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int t = 0; t < R - 1; ++t) issue(t);
+  __builtin_amdgcn_s_waitcnt(vmcnt_at_most((R - 2) * PW));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_a(a0, 0, 0);
+  read_a(a0, 0, 1);
+  read_b(b0, 0, 0);
+  for (int kt = 0; kt < KT; kt += 2) {  // KT is even
+    stage(kt, a0, b0, a1, b1);
+    stage(kt + 1, a1, b1, a0, b0);
+  }
+  // copies past the end still write this block's LDS: they land before it ends
+  __builtin_amdgcn_s_waitcnt(vmcnt_at_most(0));
+
+  // The products are transposed (weights as the first operand): lane l holds row
+  // l % 16 and columns 4 (l / 16) .. + 3 of a tile, which it stores together.
+  const int r16 = lane & 15, c4 = (lane >> 4) * 4;
+  f32x4_t t[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j) t[j] = *(const f32x4_t*)(sb + min(n0 + wn * TN + j, ns - 1) * 16 + c4);
+  const bool whole = (n0 + BN) * 16 <= N;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = (m0 + wm * TM + i) * 16 + r16;
+    if (m >= M) continue;
+    const float s = sa[m];
+    OutT* o = out + (int64_t)m * ldo + (n0 + wn * TN) * 16 + c4;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * (s * t[j][r]);
+      if (whole) {
+        store4(o + j * 16, v);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((n0 + wn * TN + j) * 16 + c4 + r < N) o[j * 16 + r] = from_f32<OutT>(v[r]);
+      }
+    }
+  }
+}
+
 template <typename OutT>
 hipError_t launch_product(const char* a, const float* sa, const char* b, const float* sb, int M,
                           int N, int KT, OutT* out, int64_t ldo, hipStream_t s) {
   const int strips = (N + 15) / 16, tiles = (M + 15) / 16;
+  if (tiles > 12) {
+    if ((long)((tiles + 15) / 16) * ((strips + 15) / 16) >= kCus) {
+      quant_tiled_kernel<16, 16, 2, 4, 4, OutT>
+          <<<dim3((tiles + 15) / 16, (strips + 15) / 16), 512, 0, s>>>(a, sa, b, sb, M, N, KT, out,
+                                                                       ldo);
+    } else {
+      quant_tiled_kernel<8, 8, 2, 2, 4, OutT>
+          <<<dim3((tiles + 7) / 8, (strips + 7) / 8), 256, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
+    }
+    return hipGetLastError();
+  }
   const dim3 grid((strips + 1) / 2, (tiles + 3) / 4);
   if (tiles == 1)
     quant_stream_kernel<1, 2, 4, OutT><<<grid, 512, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
