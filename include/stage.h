@@ -316,9 +316,13 @@ stage_status stage_quant_rows(stage_dtype dtype, const void* src, int64_t ld, in
 stage_status stage_quant_pack(const int8_t* src, int64_t ld, const float* scales, int32_t rows,
                               int32_t k, void* dst, void* stream);
 
-/* out [m, n] (row-major, stride ldo) = a b^T of two quantised matrices. */
+/* out [m, n] (row-major, stride ldo) = a b^T of two quantised matrices. ws:
+ * device scratch of stage_quant_product_bytes() bytes (0 for many sizes: ws may
+ * then be NULL), 16-byte aligned; nothing in it needs initialising. */
+size_t stage_quant_product_bytes(int32_t m, int32_t n, int32_t k);
 stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_t n, int32_t k,
-                                 stage_dtype out_dtype, void* out, int64_t ldo, void* stream);
+                                 stage_dtype out_dtype, void* out, int64_t ldo, void* ws,
+                                 size_t ws_bytes, void* stream);
 
 /* stage_lm_head with W_lm as a quantised [vocab, hidden] matrix: the normed
  * rows are quantised from float32 (they are not rounded to the mode dtype

@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libstage.so")
 ARCH = os.environ.get("STAGE_OFFLOAD_ARCH", "gfx950")
 
 SOURCES = ["k_elem.hip", "k_gemm.hip", "k_attn.hip", "k_quant.hip", "k_token.hip", "scratch.hip",
-           "stage.cpp", "store.cpp", "plan.cpp", "answer.cpp"]
+           "stage.cpp", "store.cpp", "plan.cpp", "answer.cpp", "quant_plan.cpp"]
 
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17", "-Wall",

@@ -108,8 +108,15 @@ stage_status stage_quant_pack(const int8_t* src, int64_t ld, const float* scales
   return launched("quant_pack", quant_pack(src, ld, scales, rows, k, dst, (hipStream_t)stream));
 }
 
+size_t stage_quant_product_bytes(int32_t m, int32_t n, int32_t k) {
+  if (m < 1 || n < 1 || check_matrix(m, k, "a") != STAGE_OK || check_matrix(n, k, "b") != STAGE_OK)
+    return 0;
+  return quant_plane_bytes(quant_plan(m, n, k, SIZE_MAX), m, n);
+}
+
 stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_t n, int32_t k,
-                                 stage_dtype out_dtype, void* out, int64_t ldo, void* stream) {
+                                 stage_dtype out_dtype, void* out, int64_t ldo, void* ws,
+                                 size_t ws_bytes, void* stream) {
   const int d = (int)out_dtype;
   if (!is_dtype(d)) return op_fail(STAGE_ERR_UNSUPPORTED, "dtype %d not supported", d);
   stage_status v = check_matrix(m, k, "a");
@@ -119,8 +126,10 @@ stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_
   if ((v = check_packed(a, "a")) != STAGE_OK) return v;
   if ((v = check_packed(b, "b")) != STAGE_OK) return v;
   if ((v = check_rows(out, ldo, n, esize(d), "out")) != STAGE_OK) return v;
-  return launched("quant_product",
-                  quant_product(a, m, b, n, k, (DType)d, out, ldo, (hipStream_t)stream));
+  const QuantPlan plan = quant_plan(m, n, k, SIZE_MAX);
+  if ((v = check_workspace(ws, ws_bytes, quant_plane_bytes(plan, m, n))) != STAGE_OK) return v;
+  return launched("quant_product", quant_product(plan, a, m, b, n, k, (DType)d, out, ldo, ws,
+                                                 (hipStream_t)stream));
 }
 
 stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void* w_lm,
@@ -138,7 +147,9 @@ stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void
     return quant_norm_rows(r.dt, r.hidden, r.idx, r.gain, r.eps, r.n, r.H, r.h, s);
   };
   f.product = [](const LmHeadProduct& p, const LmHeadRows& r, hipStream_t s) {
-    return quant_product(r.h, r.n, p.w, p.vocab, r.H, DT_F32, p.logits, p.vocab, s);
+    // the stage's fp32 rows are free: the normed ones went straight to 8 bits
+    const QuantPlan plan = quant_plan(r.n, p.vocab, r.H, r.x_bytes);
+    return quant_product(plan, r.h, r.n, p.w, p.vocab, r.H, DT_F32, p.logits, p.vocab, r.x, s);
   };
   f.w = w_lm;
   f.vocab = vocab;

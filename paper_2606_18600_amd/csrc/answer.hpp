@@ -36,10 +36,39 @@ hipError_t quant_pack(const int8_t* src, int64_t ld, const float* scales, int ro
 // idx[t] of src (idx: device, or nullptr for row t).
 hipError_t quant_norm_rows(DType dt, const void* src, const int32_t* idx, const void* gain,
                            float eps, int rows, int K, void* dst, hipStream_t s);
+
+// The kernels of a product (k_quant.hip): operands streamed into registers by
+// blocks of 1 or 3 strips of 16 columns; the skinny kernel with NF strips for each
+// of WC groups of waves; tiles of BM x BN strips.
+enum QuantKernel {
+  QUANT_STREAM_1,
+  QUANT_STREAM_3,
+  QUANT_SKINNY_2X2,
+  QUANT_SKINNY_4X2,
+  QUANT_SKINNY_4X4,
+  QUANT_SKINNY_4X8,
+  QUANT_TILE_16X16,
+  QUANT_TILE_8X8,
+  QUANT_TILE_4X8,
+  QUANT_TILE_4X4
+};
+constexpr int kStreamStrips = 4;   // row strips of 16 that the stream kernel takes
+constexpr int kSkinnyStrips = 12;  // ... and the skinny kernel
+// Row strips that the skinny kernel is built for: 1 and the even numbers.
+constexpr int quant_skinny_strips(int strips) { return strips <= 1 ? 1 : (strips + 1) / 2 * 2; }
+// A product's kernel and its k ranges of kt_len k tiles of 64. Several ranges
+// leave an int32 plane [M][N rounded up to 16] each, which a last kernel adds.
+struct QuantPlan {
+  QuantKernel kernel = QUANT_TILE_4X4;
+  int ranges = 1, kt_len = 0;
+};
+// The plan of a product whose planes may take `room` bytes.
+QuantPlan quant_plan(int M, int N, int K, size_t room);
+size_t quant_plane_bytes(const QuantPlan& p, int M, int N);
 // out [M, N] (fp32 or bf16, row stride ldo) = a b^T for the 8-bit matrices a
-// [M, K] and b [N, K].
-hipError_t quant_product(const void* a, int M, const void* b, int N, int K, DType out_dt,
-                         void* out, int64_t ldo, hipStream_t s);
+// [M, K] and b [N, K]; planes: quant_plane_bytes() bytes.
+hipError_t quant_product(const QuantPlan& p, const void* a, int M, const void* b, int N, int K,
+                         DType out_dt, void* out, int64_t ldo, void* planes, hipStream_t s);
 
 // probs[r] = softmax(logits[r] / temperature[r]) (temperature: device [rows],
 // nullptr for 1). ws: token_probs_bytes().

@@ -2,6 +2,7 @@
 // int8 values, exact int32 sums (v_mfma_i32_16x16x64_i8) and an fp32 scale per
 // row of either operand. Operands are in the fragment layout of answer.hpp.
 #include <algorithm>
+#include <type_traits>
 
 #include "answer.hpp"
 #include "common.hpp"
@@ -227,7 +228,13 @@ __device__ __forceinline__ void store4(bf16_t* o, const float (&v)[4]) {
   *(u32x2_any_t*)o = u32x2_any_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
-// A block owns NF strips of 16 columns and MT of 16 rows for all of K; its 8
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+// s_waitcnt immediate: at most n vector-memory operations outstanding (the
+// other counters are not waited for).
+constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+
+// A block owns NF strips of 16 columns and all rows (MT strips) for all of K; its 8
 // waves take k tiles w, w + 8, ... of 64 each, operands straight into registers
 // DEPTH tiles ahead, and add their int32 sums in LDS (integer sums do not depend
 // on their order).
@@ -240,13 +247,13 @@ void quant_stream_kernel(const char* __restrict__ A, const float* __restrict__ s
   __shared__ int red[MT * NF * 256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int strips = (N + 15) / 16;
-  const int n0 = blockIdx.x * NF, m0 = blockIdx.y * MT;
+  const int n0 = blockIdx.x * NF;
   const char* bp[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f)
     bp[f] = B + ((size_t)min(n0 + f, strips - 1) * KT + wave) * 1024 + lane * 16;
-  const char* ap = A + ((size_t)m0 * KT + wave) * 1024 + lane * 16;
-  const int left = M - m0 * 16 - (lane & 15);  // row 16 i of this lane is there if 16 i < left
+  const char* ap = A + (size_t)wave * 1024 + lane * 16;
+  const int left = M - (lane & 15);    // row 16 i of this lane is there if 16 i < left
   for (int e = threadIdx.x; e < MT * NF * 256; e += 512) red[e] = 0;
 
   i32x4_t acc[MT][NF];
@@ -256,8 +263,12 @@ void quant_stream_kernel(const char* __restrict__ A, const float* __restrict__ s
     for (int f = 0; f < NF; ++f) acc[i][f] = i32x4_t{0, 0, 0, 0};
   u32x4_t w[DEPTH][NF], a[DEPTH][MT];
   const int n = wave < KT ? (KT - wave + NW - 1) / NW : 0;
+  // Each block starts at a k tile of its own, wrapping around: in step, all blocks
+  // would ask an L2 for the same lines of A at once.
+  const int rot = n > 0 ? (int)(blockIdx.x * 7u % (unsigned)n) : 0;
   auto load = [&](int d, int t) {
     t = t < n ? t : n - 1;  // past the end: a valid tile, never used
+    t = t + rot < n ? t + rot : t + rot - n;
 #pragma unroll
     for (int f = 0; f < NF; ++f)
       w[d][f] = __builtin_nontemporal_load((const u32x4_t*)(bp[f] + (size_t)t * NW * 1024));
@@ -303,23 +314,197 @@ void quant_stream_kernel(const char* __restrict__ A, const float* __restrict__ s
   // value r of lane l of a tile: row (l / 16) * 4 + r, column l % 16
   for (int e = threadIdx.x; e < MT * NF * 256; e += 512) {
     const int c = e % (NF * 16), mr = e / (NF * 16);
-    const int m = m0 * 16 + mr, col = n0 * 16 + c;
-    if (m >= M || col >= N) continue;
+    const int col = n0 * 16 + c;
+    if (mr >= M || col >= N) continue;
     const int i = mr >> 4, f = c >> 4;
     const int v = red[((i * NF + f) * 4 + (mr & 3)) * 64 + ((mr >> 2) & 3) * 16 + (c & 15)];
-    out[(int64_t)m * ldo + col] = from_f32<OutT>((float)v * (sa[m] * sb[col]));
+    out[(int64_t)mr * ldo + col] = from_f32<OutT>((float)v * (sa[mr] * sb[col]));
+  }
+}
+
+// Wide products of few rows: 8 waves as WC groups of NF strips of columns and KP =
+// 8 / WC parts of k. Step t covers KP k tiles; a wave streams the NF weight
+// fragments of its strips and k tile into registers PF steps ahead, and all MT
+// row strips' fragments of the step, which the WC waves of a part share, go once
+// per block straight into a ring in LDS.
+template <int MT, int NF, int WC, int PF, typename OutT>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
+void quant_skinny_kernel(const char* __restrict__ A, const float* __restrict__ sa,
+                         const char* __restrict__ B, const float* __restrict__ sb, int M, int N,
+                         int KT, int kt_len, OutT* __restrict__ out, int64_t ldo) {
+  constexpr int KP = 8 / WC, AF = MT * KP, NA = (AF + 7) / 8, SLOT = NA * 8, RS = PF + 2;
+  constexpr int WAIT = vmcnt_at_most(PF * (NF + NA));
+  constexpr int RED = KP > 1 ? 8 * KP * NF * 64 : 0;  // u32x4 of the exchange at the end
+  constexpr int RING = RS * SLOT * 64;
+  __shared__ u32x4_t lds[RING > RED ? RING : RED];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wc = wave % WC, kp = wave / WC;
+  const int ms = (M + 15) / 16, ns = (N + 15) / 16;
+  const int n0 = (blockIdx.x * WC + wc) * NF;  // first strip of this wave
+  const char* bp[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) bp[f] = B + (size_t)min(n0 + f, ns - 1) * KT * 1024;
+  // fragment f of a step: k tile f / MT, row strip f % MT (copies past AF repeat the
+  // last one into places that nobody reads)
+  const char* ap[NA];
+  int ak[NA];
+#pragma unroll
+  for (int u = 0; u < NA; ++u) {
+    const int f = min(wave + 8 * u, AF - 1);
+    ap[u] = A + (size_t)min(f % MT, ms - 1) * KT * 1024;
+    ak[u] = f / MT;
+  }
+  const int k0 = blockIdx.y * kt_len, k1 = min(k0 + kt_len, KT);  // this block's k tiles
+  const int steps = (k1 - k0 + KP - 1) / KP;
+  u32x4_t w[PF + 1][NF];
+  i32x4_t acc[MT][NF];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) acc[i][f] = i32x4_t{0, 0, 0, 0};
+  // steps past the end load the last k tile again, and multiply nothing
+  auto load = [&](u32x4_t (&wf)[NF], int t) {
+    const int slot = t % RS;
+#pragma unroll
+    for (int u = 0; u < NA; ++u)
+      __builtin_amdgcn_global_load_lds(
+          (const void*)(ap[u] + (size_t)min(k0 + t * KP + ak[u], k1 - 1) * 1024 + lane * 16),
+          (lds_ptr_t)&lds[(slot * SLOT + wave + 8 * u) * 64], 16, 0, 0);
+    const size_t at = (size_t)min(k0 + t * KP + kp, k1 - 1) * 1024 + lane * 16;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      wf[f] = __builtin_nontemporal_load((const u32x4_t*)(bp[f] + at));
+  };
+  auto compute = [&](const u32x4_t (&wf)[NF], int t) {
+    const u32x4_t* a = &lds[((t % RS) * SLOT + kp * MT) * 64 + lane];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const u32x4_t ai = a[i * 64];
+#pragma unroll
+      for (int f = 0; f < NF; ++f) acc[i][f] = mfma_i8(wf[f], ai, acc[i][f]);
+    }
+  };
+#pragma unroll
+  for (int d = 0; d < PF; ++d) load(w[d], d);
+  for (int t = 0; t < steps; t += PF + 1) {
+#pragma unroll
+    for (int d = 0; d <= PF; ++d) {
+      if (t + d >= steps) break;
+      // the slot of step t + d + PF was last read in step t + d - 2, before the
+      // barrier of step t + d - 1
+      load(w[(d + PF) % (PF + 1)], t + d + PF);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(WAIT);  // this wave's loads of step t + d
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      if (KP == 1 || k0 + (t + d) * KP + kp < k1) compute(w[d], t + d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(vmcnt_at_most(0));  // copies past the end have landed too
+
+  // Lane l holds row l % 16 and columns 4 (l / 16) .. + 3 of a tile. Part q of k
+  // finishes row strips q, q + KP, ...
+  constexpr int MQ = (MT + KP - 1) / KP;
+  const int r16 = lane & 15, c4 = (lane >> 4) * 4;
+  const bool whole = (n0 + NF) * 16 <= N;
+  constexpr bool kPlane = std::is_same<OutT, int>::value;
+  f32x4_t tb[kPlane ? 1 : NF];
+  float ta[kPlane ? 1 : MQ];
+  if constexpr (kPlane) {
+    out += (size_t)blockIdx.y * M * ldo;
+  } else {
+#pragma unroll
+    for (int f = 0; f < NF; ++f) tb[f] = *(const f32x4_t*)(sb + min(n0 + f, ns - 1) * 16 + c4);
+#pragma unroll
+    for (int q = 0; q < MQ; ++q) ta[q] = sa[min((q * KP + kp) * 16 + r16, M - 1)];
+  }
+  auto store = [&](int q, const i32x4_t (&v)[NF]) {
+    const int m = (q * KP + kp) * 16 + r16;
+    if (m >= M) return;
+    OutT* o = out + (int64_t)m * ldo + n0 * 16 + c4;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      if constexpr (kPlane) {
+        if (n0 + f < ns) *(i32x4_t*)(o + f * 16) = v[f];
+      } else {
+        float x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = (float)v[f][r] * (ta[q] * tb[f][r]);
+        if (whole) {
+          store4(o + f * 16, x);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((n0 + f) * 16 + c4 + r < N) o[f * 16 + r] = from_f32<OutT>(x[r]);
+        }
+      }
+    }
+  };
+  if constexpr (KP == 1) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) store(i, acc[i]);
+  } else {
+    // KP row strips at a time: every part hands the others theirs
+#pragma unroll
+    for (int q = 0; q < MQ; ++q) {
+      __syncthreads();  // the ring, or the strips before these, have been read
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        if (q * KP + i >= MT || i == kp) continue;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+          lds[((wave * KP + i) * NF + f) * 64 + lane] =
+              __builtin_bit_cast(u32x4_t, acc[q * KP + i][f]);
+      }
+      __syncthreads();
+      i32x4_t v[NF];
+#pragma unroll
+      for (int i = 0; i < KP; ++i)
+        if (i == kp && q * KP + i < MT)
+#pragma unroll
+          for (int f = 0; f < NF; ++f) v[f] = acc[q * KP + i][f];
+#pragma unroll
+      for (int p = 0; p < KP; ++p) {
+        if (p == kp) continue;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+          v[f] += __builtin_bit_cast(i32x4_t, lds[(((p * WC + wc) * KP + kp) * NF + f) * 64 + lane]);
+      }
+      if (q * KP + kp < MT) store(q, v);
+    }
+  }
+}
+
+// out = the sum of `planes` int32 planes [M][ld] times the scales.
+template <typename OutT>
+__global__ __launch_bounds__(256) void quant_finish_kernel(const int* __restrict__ part, int planes,
+                                                           int64_t ld, const float* __restrict__ sa,
+                                                           const float* __restrict__ sb, int M,
+                                                           int N, OutT* __restrict__ out,
+                                                           int64_t ldo) {
+  const int m = blockIdx.x, n = (blockIdx.y * 256 + threadIdx.x) * 4;
+  if (n >= N) return;
+  const int* p = part + (int64_t)m * ld + n;
+  i32x4_t v = *(const i32x4_t*)p;
+  for (int q = 1; q < planes; ++q) v += *(const i32x4_t*)(p + (int64_t)q * M * ld);
+  const float s = sa[m];
+  const f32x4_t t = *(const f32x4_t*)(sb + n);
+  float o[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o[r] = (float)v[r] * (s * t[r]);
+  OutT* dst = out + (int64_t)m * ldo + n;
+  if (n + 4 <= N) {
+    store4(dst, o);
+  } else {
+    for (int r = 0; n + r < N; ++r) dst[r] = from_f32<OutT>(o[r]);
   }
 }
 
 // ---------------------------------------------------------------------------
 // many rows: tiles through LDS
 // ---------------------------------------------------------------------------
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-
-// s_waitcnt immediate: at most n vector-memory operations outstanding (the
-// other counters are not waited for).
-constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
-
 // Block tile of BM x BN strips (16 rows, 16 columns each) on WM x WN waves of
 // TM x TN. A stage is one k tile of 64: BM + BN fragments of 1 KB, copied straight
 // into a ring of R slots, R - 1 stages ahead. A wave multiplies in halves of its
@@ -336,7 +521,8 @@ constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 
 template <int BM, int BN, int WM, int WN, int R, typename OutT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
     const char* __restrict__ A, const float* __restrict__ sa, const char* __restrict__ B,
-    const float* __restrict__ sb, int M, int N, int KT, OutT* __restrict__ out, int64_t ldo) {
+    const float* __restrict__ sb, int M, int N, int KT, int kt_len, OutT* __restrict__ out,
+    int64_t ldo) {
   constexpr int NW = WM * WN, FR = BM + BN, PW = FR / NW, TM = BM / WM, TN = BN / WN, TH = TN / 2;
   static_assert(FR % NW == 0 && BM % WM == 0 && BN % WN == 0 && TN % 2 == 0, "tile split");
   __shared__ u32x4_t lds[R][FR * 64];
@@ -360,6 +546,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
   }
   const int ms = (M + 15) / 16, ns = (N + 15) / 16;
   const int m0 = mb * BM, n0 = nb * BN;
+  const int k0 = blockIdx.z * kt_len, kts = min(kt_len, KT - k0);  // this block's k tiles (even)
   // fragment f of a stage: strip m0 + f of A, then strip n0 + f - BM of B (strips
   // past the end repeat the last one; nothing of theirs is stored)
   const char* src[PW];
@@ -367,11 +554,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
   for (int p = 0; p < PW; ++p) {
     const int f = wave * PW + p;
     const size_t strip = f < BM ? min(m0 + f, ms - 1) : min(n0 + f - BM, ns - 1);
-    src[p] = (f < BM ? A : B) + strip * KT * 1024;
+    src[p] = (f < BM ? A : B) + (strip * KT + k0) * 1024;
   }
   auto issue = [&](int kt) {
     const int slot = kt % R;
-    kt = kt < KT ? kt : KT - 1;  // past the end: into a slot that nobody reads
+    kt = kt < kts ? kt : kts - 1;  // past the end: into a slot that nobody reads
 #pragma unroll
     for (int p = 0; p < PW; ++p)
       __builtin_amdgcn_global_load_lds((const void*)(src[p] + (size_t)kt * 1024 + lane * 16),
@@ -425,7 +612,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
   read_a(a0, 0, 0);
   read_a(a0, 0, 1);
   read_b(b0, 0, 0);
-  for (int kt = 0; kt < KT; kt += 2) {  // KT is even
+  for (int kt = 0; kt < kts; kt += 2) {
     stage(kt, a0, b0, a1, b1);
     stage(kt + 1, a1, b1, a0, b0);
   }
@@ -435,52 +622,136 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
   // The products are transposed (weights as the first operand): lane l holds row
   // l % 16 and columns 4 (l / 16) .. + 3 of a tile, which it stores together.
   const int r16 = lane & 15, c4 = (lane >> 4) * 4;
+  constexpr bool kPlane = std::is_same<OutT, int>::value;
+  if (kPlane) out += (size_t)blockIdx.z * M * ldo;
   f32x4_t t[TN];
+  float ta[TM];
+  if constexpr (!kPlane) {
 #pragma unroll
-  for (int j = 0; j < TN; ++j) t[j] = *(const f32x4_t*)(sb + min(n0 + wn * TN + j, ns - 1) * 16 + c4);
+    for (int j = 0; j < TN; ++j)
+      t[j] = *(const f32x4_t*)(sb + min(n0 + wn * TN + j, ns - 1) * 16 + c4);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ta[i] = sa[min((m0 + wm * TM + i) * 16 + r16, M - 1)];
+  }
   const bool whole = (n0 + BN) * 16 <= N;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = (m0 + wm * TM + i) * 16 + r16;
     if (m >= M) continue;
-    const float s = sa[m];
     OutT* o = out + (int64_t)m * ldo + (n0 + wn * TN) * 16 + c4;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      float v[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * (s * t[j][r]);
-      if (whole) {
-        store4(o + j * 16, v);
+      if constexpr (kPlane) {
+        if (n0 + wn * TN + j < ns) *(i32x4_t*)(o + j * 16) = acc[i][j];
       } else {
+        float v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if ((n0 + wn * TN + j) * 16 + c4 + r < N) o[j * 16 + r] = from_f32<OutT>(v[r]);
+        for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][r] * (ta[i] * t[j][r]);
+        if (whole) {
+          store4(o + j * 16, v);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((n0 + wn * TN + j) * 16 + c4 + r < N) o[j * 16 + r] = from_f32<OutT>(v[r]);
+        }
       }
     }
   }
 }
 
-template <typename OutT>
-hipError_t launch_product(const char* a, const float* sa, const char* b, const float* sb, int M,
-                          int N, int KT, OutT* out, int64_t ldo, hipStream_t s) {
-  const int strips = (N + 15) / 16, tiles = (M + 15) / 16;
-  if (tiles > 12) {
-    if ((long)((tiles + 15) / 16) * ((strips + 15) / 16) >= kCus) {
-      quant_tiled_kernel<16, 16, 2, 4, 4, OutT>
-          <<<dim3((tiles + 15) / 16, (strips + 15) / 16), 512, 0, s>>>(a, sa, b, sb, M, N, KT, out,
-                                                                       ldo);
-    } else {
-      quant_tiled_kernel<8, 8, 2, 2, 4, OutT>
-          <<<dim3((tiles + 7) / 8, (strips + 7) / 8), 256, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
-    }
-    return hipGetLastError();
+struct Product {
+  const char* a;
+  const float* sa;
+  const char* b;
+  const float* sb;
+  int M, N, KT;
+  QuantPlan plan;
+  int* planes;
+  hipStream_t s;
+};
+
+template <int MT, int NF, typename OutT>
+void launch_stream(const Product& p, OutT* out, int64_t ldo) {
+  constexpr int DEPTH = NF == 1 ? 4 : 3;
+  const int strips = (p.N + 15) / 16;
+  quant_stream_kernel<MT, NF, DEPTH, OutT><<<(strips + NF - 1) / NF, 512, 0, p.s>>>(
+      p.a, p.sa, p.b, p.sb, p.M, p.N, p.KT, out, ldo);
+}
+
+// Two steps ahead where many waves share the rows and the sums leave registers
+// for it (64 rows: N = 57344 79.8 -> 76.8 us, 128256 169 -> 158; 128 rows of 57344
+// on 4 x 4 79.8 -> 87.4).
+template <int MT, int NF, int WC, typename OutT>
+void launch_skinny(const Product& p, OutT* out, int64_t ldo) {
+  constexpr int PF = MT <= 4 && WC >= 4 ? 2 : 1;
+  const int strips = (p.N + 15) / 16;
+  quant_skinny_kernel<MT, NF, WC, PF, OutT>
+      <<<dim3((strips + NF * WC - 1) / (NF * WC), p.plan.ranges), 512, 0, p.s>>>(
+          p.a, p.sa, p.b, p.sb, p.M, p.N, p.KT, p.plan.kt_len, out, ldo);
+}
+
+template <int BM, int BN, int WM, int WN, int R, typename OutT>
+void launch_tiled(const Product& p, OutT* out, int64_t ldo) {
+  const int strips = (p.N + 15) / 16, tiles = (p.M + 15) / 16;
+  quant_tiled_kernel<BM, BN, WM, WN, R, OutT>
+      <<<dim3((tiles + BM - 1) / BM, (strips + BN - 1) / BN, p.plan.ranges), WM * WN * 64, 0,
+         p.s>>>(p.a, p.sa, p.b, p.sb, p.M, p.N, p.KT, p.plan.kt_len, out, ldo);
+}
+
+template <int NF, int WC, typename OutT>
+void launch_skinny_rows(const Product& p, OutT* out, int64_t ldo) {
+  switch (quant_skinny_strips((p.M + 15) / 16)) {
+    case 1:
+      if constexpr (WC < 8) launch_skinny<1, NF, WC>(p, out, ldo);
+      break;
+    case 2: launch_skinny<2, NF, WC>(p, out, ldo); break;
+    case 4: launch_skinny<4, NF, WC>(p, out, ldo); break;
+    case 6: launch_skinny<6, NF, WC>(p, out, ldo); break;
+    case 8: launch_skinny<8, NF, WC>(p, out, ldo); break;
+    case 10: launch_skinny<10, NF, WC>(p, out, ldo); break;
+    default: launch_skinny<12, NF, WC>(p, out, ldo);
   }
-  const dim3 grid((strips + 1) / 2, (tiles + 3) / 4);
+}
+
+template <typename OutT>
+void launch_ranges(const Product& p, OutT* out, int64_t ldo) {
+  switch (p.plan.kernel) {
+    case QUANT_SKINNY_2X2: launch_skinny_rows<2, 2>(p, out, ldo); break;
+    case QUANT_SKINNY_4X2: launch_skinny_rows<4, 2>(p, out, ldo); break;
+    case QUANT_SKINNY_4X4: launch_skinny_rows<4, 4>(p, out, ldo); break;
+    case QUANT_SKINNY_4X8: launch_skinny_rows<4, 8>(p, out, ldo); break;
+    case QUANT_TILE_16X16: launch_tiled<16, 16, 2, 4, 4>(p, out, ldo); break;
+    case QUANT_TILE_8X8: launch_tiled<8, 8, 2, 2, 5>(p, out, ldo); break;
+    case QUANT_TILE_4X8: launch_tiled<4, 8, 2, 2, 6>(p, out, ldo); break;
+    default: launch_tiled<4, 4, 2, 2, 8>(p, out, ldo);
+  }
+}
+
+template <int NF, typename OutT>
+void launch_stream_rows(const Product& p, OutT* out, int64_t ldo) {
+  const int tiles = (p.M + 15) / 16;
   if (tiles == 1)
-    quant_stream_kernel<1, 2, 4, OutT><<<grid, 512, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
+    launch_stream<1, NF>(p, out, ldo);
+  else if (tiles == 2)
+    launch_stream<2, NF>(p, out, ldo);
   else
-    quant_stream_kernel<4, 2, 2, OutT><<<grid, 512, 0, s>>>(a, sa, b, sb, M, N, KT, out, ldo);
+    launch_stream<4, NF>(p, out, ldo);
+}
+
+template <typename OutT>
+hipError_t launch_product(const Product& p, OutT* out, int64_t ldo) {
+  if (p.plan.kernel == QUANT_STREAM_1) {
+    launch_stream_rows<1>(p, out, ldo);
+  } else if (p.plan.kernel == QUANT_STREAM_3) {
+    launch_stream_rows<3>(p, out, ldo);
+  } else if (p.plan.ranges == 1) {
+    launch_ranges(p, out, ldo);
+  } else {
+    const int64_t ld = (p.N + 15) / 16 * 16;
+    launch_ranges(p, p.planes, ld);
+    quant_finish_kernel<OutT><<<dim3(p.M, (p.N + 1023) / 1024), 256, 0, p.s>>>(
+        p.planes, p.plan.ranges, ld, p.sa, p.sb, p.M, p.N, out, ldo);
+  }
   return hipGetLastError();
 }
 
@@ -538,16 +809,15 @@ hipError_t quant_norm_rows(DType dt, const void* src, const int32_t* idx, const 
   return hipGetLastError();
 }
 
-hipError_t quant_product(const void* a, int M, const void* b, int N, int K, DType out_dt,
-                         void* out, int64_t ldo, hipStream_t s) {
+hipError_t quant_product(const QuantPlan& plan, const void* a, int M, const void* b, int N, int K,
+                         DType out_dt, void* out, int64_t ldo, void* planes, hipStream_t s) {
   if (M == 0) return hipSuccess;
   const char *ac = (const char*)a, *bc = (const char*)b;
-  const float* sa = (const float*)(ac + quant_scales_at(M, K));
-  const float* sb = (const float*)(bc + quant_scales_at(N, K));
-  const int KT = (int)(quant_kp(K) / 64);
-  if (out_dt == DT_F32)
-    return launch_product(ac, sa, bc, sb, M, N, KT, (float*)out, ldo, s);
-  return launch_product(ac, sa, bc, sb, M, N, KT, (bf16_t*)out, ldo, s);
+  const Product p{ac, (const float*)(ac + quant_scales_at(M, K)),
+                  bc, (const float*)(bc + quant_scales_at(N, K)),
+                  M,  N, (int)(quant_kp(K) / 64), plan, (int*)planes, s};
+  if (out_dt == DT_F32) return launch_product(p, (float*)out, ldo);
+  return launch_product(p, (bf16_t*)out, ldo);
 }
 
 }  // namespace stage_k

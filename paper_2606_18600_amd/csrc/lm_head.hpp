@@ -19,7 +19,7 @@ struct LmHeadRows {
   float eps = 0.f;
   float* x = nullptr;
   void* h = nullptr;
-  size_t h_bytes = 0;
+  size_t x_bytes = 0, h_bytes = 0;
   int skinny_rows = 0;
 };
 

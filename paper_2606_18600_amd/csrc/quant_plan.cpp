@@ -1,0 +1,116 @@
+// Which kernel an 8-bit product runs on, and over how many k ranges. Plain host
+// code (no HIP calls).
+//
+// The candidates' times are estimated and the least is taken. The estimate has
+// three parts, in us, with constants fitted to 2100 timings of 126 sizes (1 to 3000
+// rows, 64 to 57344 columns, k of 128 to 28672); over those sizes the choice is
+// on average 1.2% and at worst 13% slower than the fastest candidate:
+//  - reading the operands from HBM at the rate that the kernel reaches;
+//  - what one CU has to load (few rows) or multiply (tiles) for its share of the
+//    blocks, which is what decides among them;
+//  - with several k ranges, writing and adding their int32 planes.
+// What the candidates are for, each against the next best one in us:
+//   stream, 1 strip     7 x 3712 x 11264        9.8 (tiles of 4 x 4, 4 ranges: 11.7)
+//   stream, 3 strips    2 x 10368 x 9570       17.4 (stream, 1 strip: 19.0)
+//   skinny, 2 x 2       128 x 10240 x 5120     20.6 (tiles of 4 x 8: 21.4)
+//   skinny, 4 x 2       150 x 8192 x 28672     56.9 (skinny 4 x 4, 8 ranges: 58.2)
+//   skinny, 4 x 4       64 x 57344 x 8192      76.8 (skinny 4 x 2: 86.8)
+//   skinny, 4 x 8       64 x 128256 x 8192    158.3 (skinny 4 x 4: 184.9)
+//   tiles, 4 x 4        613 x 1277 x 2503       8.8 (tiles of 4 x 8: 11.6)
+//   tiles, 4 x 8        150 x 10240 x 5120     20.4 (skinny 2 x 2: 24.4)
+//   tiles, 8 x 8        2048 x 2048 x 2048     12.6 (tiles of 4 x 8: 14.2)
+//   tiles, 16 x 16      2048 x 57344 x 8192     735 (tiles of 8 x 8: 958)
+#include <algorithm>
+
+#include "answer.hpp"
+
+namespace stage_k {
+
+namespace {
+
+long up(long a, long b) { return (a + b - 1) / b; }
+
+// A tile kernel: its strips, ring slots, and the time of a stage with one block on
+// a CU and with two (0: its LDS allows one), and of its ends.
+struct Tile {
+  QuantKernel kind;
+  int bm, bn, ring;
+  double one, two, ends;
+};
+constexpr Tile kTiles[] = {{QUANT_TILE_16X16, 16, 16, 4, 0.75, 0.0, 0.0},
+                           {QUANT_TILE_8X8, 8, 8, 5, 0.22, 0.51, 1.1},
+                           {QUANT_TILE_4X8, 4, 8, 6, 0.137, 0.36, 0.9},
+                           {QUANT_TILE_4X4, 4, 4, 8, 0.087, 0.22, 0.8}};
+struct Skinny {
+  QuantKernel kind;
+  int nf, wc;
+};
+constexpr Skinny kSkinny[] = {{QUANT_SKINNY_2X2, 2, 2},
+                              {QUANT_SKINNY_4X2, 4, 2},
+                              {QUANT_SKINNY_4X4, 4, 4},
+                              {QUANT_SKINNY_4X8, 4, 8}};
+constexpr int kRanges[] = {1, 2, 3, 4, 6, 8};
+
+}  // namespace
+
+size_t quant_plane_bytes(const QuantPlan& p, int M, int N) {
+  return p.ranges > 1 ? (size_t)p.ranges * M * quant_rows16(N) * 4 : 0;
+}
+
+QuantPlan quant_plan(int M, int N, int K, size_t room) {
+  const long strips = up(N, 16), tiles = up(M, 16), KT = (long)quant_kp(K) / 64;
+  const double mb = ((double)N * K + (double)M * K + (double)M * N * 2) * 1e-6;
+  const double weights = (double)N * K;
+  QuantPlan best;
+  double least = 1e30;
+  auto offer = [&](QuantKernel kind, long kt_len, double us) {
+    QuantPlan p;
+    p.kernel = kind;
+    p.kt_len = (int)kt_len;
+    p.ranges = (int)up(KT, kt_len);
+    if (p.ranges > 1) {
+      const size_t bytes = quant_plane_bytes(p, M, N);
+      if (bytes > room) return;
+      us += 2.0 + bytes / 2.43e6;
+    }
+    if (us < least) least = us, best = p;
+  };
+  if (tiles <= kStreamStrips)
+    for (int nf : {1, 3}) {
+      const long rounds = up(up(strips, nf), kCus);
+      offer(nf == 1 ? QUANT_STREAM_1 : QUANT_STREAM_3, KT,
+            std::max(mb / 6.6, rounds * KT * (M / 16.0 + nf) / 48.5) + 0.28 * rounds);
+    }
+  if (tiles <= kSkinnyStrips) {
+    const long mt = quant_skinny_strips((int)tiles);
+    for (const Skinny& k : kSkinny) {
+      if (k.wc == 8 && tiles == 1) continue;
+      const int kp = 8 / k.wc, cols = k.nf * k.wc;
+      for (int r : kRanges) {
+        const long len = up(up(KT, r), kp) * kp;
+        if (up(KT, len) != r) continue;
+        const long rounds = up(up(strips, cols) * r, kCus);
+        offer(k.kind, len,
+              std::max(mb / 6.55 * (1 + 0.23 * mt / cols), rounds * len * (mt + cols) / 49.8) +
+                  0.3 * rounds);
+      }
+    }
+  }
+  for (const Tile& t : kTiles)
+    for (int r : kRanges) {
+      const long len = up(up(KT, r), 2) * 2;
+      if (r == 6 || up(KT, len) != r) continue;
+      // weights too large for the memory-side cache arrive no sooner than HBM's latency
+      const double slow = weights > 4e7 ? 1.02 / (t.ring - 1) : 0.0;
+      const double one = std::max(t.one, slow), two = std::max(t.two, one);
+      const long per = t.two > 0 ? 2 * kCus : kCus;
+      const long blocks = up(tiles, t.bm) * up(strips, t.bn) * r;
+      const long full = blocks / per, rest = blocks % per;
+      double us = full * (len * (t.two > 0 ? two : one) + t.ends);
+      if (rest) us += len * (rest > kCus ? two : one) + t.ends;
+      offer(t.kind, len, std::max(us, mb / 5.5));
+    }
+  return best;
+}
+
+}  // namespace stage_k

@@ -842,6 +842,7 @@ stage_status stage_k::lm_head_rows(stage* st, const LmHeadProduct& f, const void
   r.eps = c.rms_eps;
   r.x = st->at<float>(st->r_x);
   r.h = st->ws + st->r_h.off;
+  r.x_bytes = st->r_x.bytes;
   r.h_bytes = st->r_h.bytes;
   r.skinny_rows = st->skinny_rows;
   Launcher L{st, s};

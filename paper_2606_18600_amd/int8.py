@@ -155,8 +155,11 @@ def product(a: Matrix, b: Matrix, dtype: torch.dtype = torch.bfloat16,
     with at_device(device) as stream:
         if out is None:
             out = torch.empty((a.rows, b.rows), dtype=dtype, device=device)
+        size = S.stage_quant_product_bytes(a.rows, b.rows, a.k)
+        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
         S.stage_quant_product(a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows, a.k, dt,
-                              out.data_ptr(), row_stride(out), stream)
+                              out.data_ptr(), row_stride(out),
+                              None if ws is None else ws.data_ptr(), size, stream)
     return out
 
 

@@ -70,15 +70,17 @@ def test_quant_pack_refuses(args, code):
     ((A, 4, B, 8, 200000, F32, C, 8), UNS),
 ])
 def test_quant_product_refuses(args, code):
-    _refused(_lib().stage_quant_product(*args, None), code)
+    _refused(_lib().stage_quant_product(*args, None, 0, None), code)
 
 
 def test_empty_calls_do_nothing():
     lib = _lib()
     assert lib.stage_quant_rows(F32, None, 0, 0, 64, None, None) == S.STAGE_OK
     assert lib.stage_quant_pack(None, 0, None, 0, 64, None, None) == S.STAGE_OK
-    assert lib.stage_quant_product(None, 0, None, 8, 64, F32, None, 8, None) == S.STAGE_OK
-    assert lib.stage_quant_product(None, 8, None, 0, 64, F32, None, 0, None) == S.STAGE_OK
+    assert lib.stage_quant_product(None, 0, None, 8, 64, F32, None, 8, None, 0,
+                                   None) == S.STAGE_OK
+    assert lib.stage_quant_product(None, 8, None, 0, 64, F32, None, 0, None, 0,
+                                   None) == S.STAGE_OK
     assert lib.stage_token_probs(F32, None, 0, 0, 64, None, F32, None, 0, None, 0,
                                  None) == S.STAGE_OK
     empty = S.stage_drafts(F32, 64, 0, 0, 4)
@@ -108,6 +110,11 @@ def test_token_probs_refuses(args, code):
 
 def test_workspaces_are_checked():
     lib = _lib()
+    need = S.stage_quant_product_bytes(128, 1280, 8192)   # a product over several k ranges
+    assert need > 0 and S.stage_quant_product_bytes(0, 1280, 8192) == 0
+    assert S.stage_quant_product_bytes(4, 8, 0) == 0
+    for ws, size, code in ((0, need, INV), (D, need - 1, CAP), (D + 8, need, INV)):
+        _refused(lib.stage_quant_product(A, 128, B, 1280, 8192, F32, C, 1280, ws, size, None), code)
     need = S.stage_token_probs_bytes(2, 100000)
     assert need > 0 and S.stage_token_probs_bytes(2, 0) == 0
     for ws, size, code in ((0, need, INV), (D, need - 1, CAP), (D + 8, need, INV)):

@@ -90,6 +90,23 @@ def test_linear_wide_and_deep(m):
     _close(y[:, cols], _reference(x, w[cols]), "f32")
 
 
+@pytest.mark.parametrize("m,n,k", [
+    (1, 57339, 700), (2, 50001, 3001), (16, 28671, 8192), (9, 128251, 130), (20, 57339, 1100),
+    (33, 57339, 2000), (64, 10239, 5120), (64, 128251, 1000), (70, 128251, 250), (100, 57339, 2000),
+    (125, 128251, 900), (128, 10239, 5120), (128, 8191, 8192), (130, 57339, 2000),
+    (150, 28670, 4096), (165, 57339, 515), (190, 128251, 700), (40, 5121, 20000),
+    (10, 12930, 9000), (1100, 40961, 200), (2050, 8200, 300), (2100, 20001, 160)])
+def test_linear_many_columns(m, n, k):
+    """Sizes that keep most of the chip at work, one or more for each kernel; all rows,
+    a sample of columns with the first and the last."""
+    x, w = _draw(m, m, k, "bf16"), _draw(n, n, k, "bf16")
+    y = int8.linear(x, int8.quantize(w), torch.float32)
+    assert y.shape == (m, n) and y.isfinite().all()
+    cols = torch.cat([torch.arange(0, n, max(1, n // 150), device="cuda"),
+                      torch.arange(n - 40, n, device="cuda")])
+    _close(y[:, cols], _reference(x, w[cols]), "f32")
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 40, 200), (70, 100, 384), (300, 520, 256), (1030, 64, 130)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_and_addresses(m, n, k, dtype):
