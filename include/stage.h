@@ -324,6 +324,14 @@ stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_
                                  stage_dtype out_dtype, void* out, int64_t ldo, void* ws,
                                  size_t ws_bytes, void* stream);
 
+/* out [m, n] = x w^T for activations x [m, k] of `dtype` and a quantised w [n,
+ * k]: stage_quant_rows into the scratch, then stage_quant_product, in one call. ws:
+ * stage_quant_linear_bytes() bytes, as above. */
+size_t stage_quant_linear_bytes(int32_t m, int32_t n, int32_t k);
+stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, int32_t m, int32_t k,
+                                const void* w, int32_t n, stage_dtype out_dtype, void* out,
+                                int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
 /* stage_lm_head with W_lm as a quantised [vocab, hidden] matrix: the normed
  * rows are quantised from float32 (they are not rounded to the mode dtype
  * first). Any vocab >= 1; everything else as for stage_lm_head, the pointers

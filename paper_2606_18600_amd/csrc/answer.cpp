@@ -40,6 +40,8 @@ bool at_multiple(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 size_t esize(int d) { return d == STAGE_F32 ? 4 : 2; }
 
+size_t align16(size_t n) { return (n + 15) / 16 * 16; }
+
 // A quantised matrix's size, as every call checks it.
 stage_status check_matrix(int32_t rows, int32_t k, const char* what) {
   if (rows < 0 || k < 1)
@@ -130,6 +132,35 @@ stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_
   if ((v = check_workspace(ws, ws_bytes, quant_plane_bytes(plan, m, n))) != STAGE_OK) return v;
   return launched("quant_product", quant_product(plan, a, m, b, n, k, (DType)d, out, ldo, ws,
                                                  (hipStream_t)stream));
+}
+
+size_t stage_quant_linear_bytes(int32_t m, int32_t n, int32_t k) {
+  if (m < 1 || n < 1 || check_matrix(m, k, "x") != STAGE_OK || check_matrix(n, k, "w") != STAGE_OK)
+    return 0;
+  return align16(quant_bytes(m, k)) + quant_plane_bytes(quant_plan(m, n, k, SIZE_MAX), m, n);
+}
+
+stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, int32_t m, int32_t k,
+                                const void* w, int32_t n, stage_dtype out_dtype, void* out,
+                                int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
+  const int d = (int)dtype, o = (int)out_dtype;
+  if (!is_dtype(d) || !is_dtype(o))
+    return op_fail(STAGE_ERR_UNSUPPORTED, "dtypes %d, %d not supported", d, o);
+  stage_status v = check_matrix(m, k, "x");
+  if (v != STAGE_OK) return v;
+  if ((v = check_matrix(n, k, "w")) != STAGE_OK) return v;
+  if (m == 0 || n == 0) return STAGE_OK;
+  if ((v = check_rows(x, ld, k, esize(d), "x")) != STAGE_OK) return v;
+  if ((v = check_packed(w, "w")) != STAGE_OK) return v;
+  if ((v = check_rows(out, ldo, n, esize(o), "out")) != STAGE_OK) return v;
+  const QuantPlan plan = quant_plan(m, n, k, SIZE_MAX);
+  const size_t planes = align16(quant_bytes(m, k));
+  if ((v = check_workspace(ws, ws_bytes, planes + quant_plane_bytes(plan, m, n))) != STAGE_OK)
+    return v;
+  hipStream_t s = (hipStream_t)stream;
+  if ((v = launched("quant_rows", quant_rows((DType)d, x, ld, m, k, ws, s))) != STAGE_OK) return v;
+  return launched("quant_product", quant_product(plan, ws, m, w, n, k, (DType)o, out, ldo,
+                                                 (char*)ws + planes, s));
 }
 
 stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void* w_lm,

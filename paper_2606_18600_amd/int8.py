@@ -1,9 +1,10 @@
 """Products in 8-bit integers over torch tensors (``stage_quant_*`` of the ABI).
 
 ``quantize`` turns the rows of a matrix into 8-bit integers with a scale each:
-activations before a product, or weights once, when they are loaded
-(``pack_weight`` takes weights that are in 8 bits already). ``product`` multiplies
-two of them, ``linear`` quantises activations and multiplies in one call::
+weights once, when they are loaded (``pack_weight`` takes weights that are in 8 bits
+already), or activations that several products share. ``linear`` quantises
+activations and multiplies in one call, ``product`` multiplies two quantised
+matrices::
 
     w = int8.quantize(weight)            # [n, k] bf16 or fp32, once
     y = int8.linear(x, w)                # [..., k] -> [..., n]
@@ -16,7 +17,7 @@ may be captured into a graph.
 
 from __future__ import annotations
 
-from dataclasses import dataclass
+from functools import lru_cache
 from typing import Optional
 
 import torch
@@ -49,36 +50,32 @@ def on_gpu(*tensors: Optional[torch.Tensor]) -> torch.device:
     return device
 
 
-class at_device:
-    """Makes ``device`` current, where it is not, for the calls of a block and
-    gives torch's current stream on it."""
+def is_current(device: torch.device) -> bool:
+    """Whether the library's calls would run on this GPU: they go to the current
+    one. Callers make it so with ``torch.cuda.device``."""
+    return torch.cuda.current_device() == device.index
 
-    __slots__ = ("device", "guard")
 
-    def __init__(self, device: torch.device):
-        self.device, self.guard = device, None
+def stream_of(device: torch.device) -> int:
+    """torch's current stream on a GPU. (The public call builds a Stream object,
+    3 us of a launch-bound call.)"""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
-    def __enter__(self) -> int:
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
 
-    def __exit__(self, *exc) -> None:
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def scratch(n: int, device: torch.device) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.uint8, device=device)
 
 
 def rows_of(x: torch.Tensor, what: str) -> torch.Tensor:
     """x as [rows, k] with adjacent values in a row."""
-    if x.dim() == 0:
-        raise invalid(f"{what} has no dimension")
     if x.dim() != 2:
+        if x.dim() == 0:
+            raise invalid(f"{what} has no dimension")
         x = x.reshape(-1, x.shape[-1])
-    if x.shape[1] > 1 and x.stride(1) != 1:
-        x = x.contiguous()
-    elif x.shape[0] > 1 and x.stride(0) < x.shape[1]:
-        x = x.contiguous()  # rows that overlap (an expanded tensor)
+    if not x.is_contiguous():
+        rows, k = x.shape
+        if (k > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < k):
+            x = x.contiguous()  # transposed, or rows that overlap (an expanded tensor)
     return x
 
 
@@ -86,25 +83,36 @@ def row_stride(x: torch.Tensor) -> int:
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
-@dataclass(frozen=True)
+def check_out(out: torch.Tensor, rows: int, cols: int) -> None:
+    if out.shape != (rows, cols) or (out.numel() and cols > 1 and out.stride(1) != 1) or \
+            (rows > 1 and out.stride(0) < cols):
+        raise invalid(f"out must be [{rows}, {cols}] with adjacent columns, not "
+                      f"{tuple(out.shape)} with strides {out.stride()}")
+
+
 class Matrix:
     """A quantised [rows, k] matrix: opaque device memory of its values and
     scales."""
 
-    data: torch.Tensor
-    rows: int
-    k: int
+    __slots__ = ("data", "rows", "k")
+
+    def __init__(self, data: torch.Tensor, rows: int, k: int):
+        self.data, self.rows, self.k = data, rows, k
 
     @property
     def shape(self):
         return (self.rows, self.k)
 
 
+_product_bytes = lru_cache(4096)(S.stage_quant_product_bytes)
+_linear_bytes = lru_cache(4096)(S.stage_quant_linear_bytes)
+
+
 def _empty(rows: int, k: int, device) -> torch.Tensor:
     n = S.stage_quant_bytes(rows, k)
     if n == 0 and rows > 0:
         raise S.StageError(S.STAGE_ERR_UNSUPPORTED, S.stage_last_error())
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return scratch(n, device)
 
 
 def quantize(x: torch.Tensor) -> Matrix:
@@ -114,11 +122,13 @@ def quantize(x: torch.Tensor) -> Matrix:
     if dt is None:
         raise unsupported(f"quantize: {x.dtype}")
     device = on_gpu(x)
+    if not is_current(device):
+        with torch.cuda.device(device):
+            return quantize(x)
     x = rows_of(x, "x")
     m, k = x.shape
-    with at_device(device) as stream:
-        data = _empty(m, k, device)
-        S.stage_quant_rows(dt, x.data_ptr(), row_stride(x), m, k, data.data_ptr(), stream)
+    data = _empty(m, k, device)
+    S.stage_quant_rows(dt, x.data_ptr(), row_stride(x), m, k, data.data_ptr(), stream_of(device))
     return Matrix(data, m, k)
 
 
@@ -129,45 +139,63 @@ def pack_weight(values: torch.Tensor, scales: torch.Tensor) -> Matrix:
     if scales.dtype != torch.float32 or scales.shape != values.shape[:1]:
         raise invalid("pack_weight: scales must be float32 [n]")
     device = on_gpu(values, scales)
+    if not is_current(device):
+        with torch.cuda.device(device):
+            return pack_weight(values, scales)
     values, scales = rows_of(values, "values"), scales.contiguous()
     n, k = values.shape
-    with at_device(device) as stream:
-        data = _empty(n, k, device)
-        S.stage_quant_pack(values.data_ptr(), row_stride(values), scales.data_ptr(), n, k,
-                           data.data_ptr(), stream)
+    data = _empty(n, k, device)
+    S.stage_quant_pack(values.data_ptr(), row_stride(values), scales.data_ptr(), n, k,
+                       data.data_ptr(), stream_of(device))
     return Matrix(data, n, k)
 
 
 def product(a: Matrix, b: Matrix, dtype: torch.dtype = torch.bfloat16,
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """a b^T [a.rows, b.rows] in ``dtype``, or into ``out`` (any row stride)."""
-    if a.k != b.k:
+    m, n, k = a.rows, b.rows, a.k
+    if k != b.k:
         raise invalid(f"product of {a.shape} and {b.shape}")
     device = on_gpu(a.data, b.data, out)
+    if not is_current(device):
+        with torch.cuda.device(device):
+            return product(a, b, dtype, out)
     if out is not None:
+        check_out(out, m, n)
         dtype = out.dtype
-        if out.shape != (a.rows, b.rows) or (out.numel() and b.rows > 1 and out.stride(1) != 1) or \
-                (a.rows > 1 and out.stride(0) < b.rows):
-            raise invalid(f"product: out {tuple(out.shape)} with strides {out.stride()}")
     dt = DTYPES.get(dtype)
     if dt is None:
         raise unsupported(f"product: {dtype}")
-    with at_device(device) as stream:
-        if out is None:
-            out = torch.empty((a.rows, b.rows), dtype=dtype, device=device)
-        size = S.stage_quant_product_bytes(a.rows, b.rows, a.k)
-        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-        S.stage_quant_product(a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows, a.k, dt,
-                              out.data_ptr(), row_stride(out),
-                              None if ws is None else ws.data_ptr(), size, stream)
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=device)
+    size = _product_bytes(m, n, k)
+    ws = scratch(size, device).data_ptr() if size else None
+    S.stage_quant_product(a.data.data_ptr(), m, b.data.data_ptr(), n, k, dt, out.data_ptr(),
+                          row_stride(out), ws, size, stream_of(device))
     return out
 
 
 def linear(x: torch.Tensor, w: Matrix, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """x [..., k] (fp32 or bf16) times w [n, k] transposed: [..., n] in ``dtype``
     (x's own unless given)."""
-    if x.dim() == 0 or x.shape[-1] != w.k:
+    n, k = w.rows, w.k
+    if x.dim() == 0 or x.shape[-1] != k:
         raise invalid(f"linear: {tuple(x.shape)} times {w.shape}")
-    on_gpu(x, w.data)
-    y = product(quantize(x), w, x.dtype if dtype is None else dtype)
-    return y if x.dim() == 2 else y.view(*x.shape[:-1], w.rows)
+    if dtype is None:
+        dtype = x.dtype
+    dt, dt_out = DTYPES.get(x.dtype), DTYPES.get(dtype)
+    if dt is None or dt_out is None:
+        raise unsupported(f"linear: {x.dtype} to {dtype}")
+    device = on_gpu(x, w.data)
+    if not is_current(device):
+        with torch.cuda.device(device):
+            return linear(x, w, dtype)
+    shape = x.shape
+    x = rows_of(x, "x")
+    m = x.shape[0]
+    y = torch.empty((m, n), dtype=dtype, device=device)
+    size = _linear_bytes(m, n, k)
+    ws = scratch(size, device)
+    S.stage_quant_linear(dt, x.data_ptr(), row_stride(x), m, k, w.data.data_ptr(), n, dt_out,
+                         y.data_ptr(), n, ws.data_ptr(), size, stream_of(device))
+    return y if len(shape) == 2 else y.view(*shape[:-1], n)

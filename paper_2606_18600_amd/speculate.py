@@ -15,12 +15,17 @@ torch's allocator, so calls may be captured into a graph.
 
 from __future__ import annotations
 
+from functools import lru_cache
 from typing import Optional, Tuple
 
 import torch
 
 from . import stage as S
-from .int8 import DTYPES, at_device, invalid, on_gpu, row_stride, rows_of, unsupported
+from .int8 import (DTYPES, check_out, invalid, is_current, on_gpu, row_stride, rows_of, scratch,
+                   stream_of, unsupported)
+
+_probs_bytes = lru_cache(4096)(S.stage_token_probs_bytes)
+_verify_bytes = lru_cache(4096)(S.stage_verify_bytes)
 
 
 def token_probs(logits: torch.Tensor, temperature: Optional[torch.Tensor] = None,
@@ -30,32 +35,34 @@ def token_probs(logits: torch.Tensor, temperature: Optional[torch.Tensor] = None
     fp32 or bf16; temperature fp32, one per row (None: 1; 0: the largest logit,
     the lowest token among equals). The result is in ``dtype``, or in ``out``
     ([rows, vocab], any row stride), which may be the logits themselves."""
-    dt = DTYPES.get(logits.dtype)
-    dt_out = DTYPES.get(dtype if out is None else out.dtype)
+    if out is not None:
+        dtype = out.dtype
+    dt, dt_out = DTYPES.get(logits.dtype), DTYPES.get(dtype)
     if dt is None or dt_out is None:
-        raise unsupported(f"token_probs: {logits.dtype} to {dtype if out is None else out.dtype}")
+        raise unsupported(f"token_probs: {logits.dtype} to {dtype}")
     device = on_gpu(logits, temperature, out)
+    if not is_current(device):
+        with torch.cuda.device(device):
+            return token_probs(logits, temperature, dtype, out)
     shape = logits.shape
     logits = rows_of(logits, "logits")
     rows, vocab = logits.shape
+    t = None
     if temperature is not None:
         if temperature.dtype != torch.float32 or temperature.numel() != rows:
             raise invalid(f"temperature must be float32, one for each of {rows} rows")
         temperature = temperature.reshape(-1).contiguous()
-    if out is not None and (out.shape != (rows, vocab) or (vocab > 1 and out.stride(1) != 1) or
-                            (rows > 1 and out.stride(0) < vocab)):
-        raise invalid(f"out {tuple(out.shape)} with strides {out.stride()}")
-    with at_device(device) as stream:
-        if out is None:
-            out = torch.empty((rows, vocab), dtype=dtype, device=device)
-            result = out if len(shape) == 2 else out.view(shape)
-        else:
-            result = out
-        size = S.stage_token_probs_bytes(rows, vocab)
-        ws = torch.empty(size, dtype=torch.uint8, device=device)
-        S.stage_token_probs(dt, logits.data_ptr(), row_stride(logits), rows, vocab,
-                            None if temperature is None else temperature.data_ptr(), dt_out,
-                            out.data_ptr(), row_stride(out), ws.data_ptr(), size, stream)
+        t = temperature.data_ptr()
+    if out is None:
+        y = torch.empty((rows, vocab), dtype=dtype, device=device)
+        result = y if len(shape) == 2 else y.view(shape)
+    else:
+        check_out(out, rows, vocab)
+        y = result = out
+    size = _probs_bytes(rows, vocab)
+    ws = scratch(size, device).data_ptr() if size else None
+    S.stage_token_probs(dt, logits.data_ptr(), row_stride(logits), rows, vocab, t, dt_out,
+                        y.data_ptr(), row_stride(y), ws, size, stream_of(device))
     return result
 
 
@@ -83,6 +90,10 @@ def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor
     if target_probs.dim() != 2 or drafts.dim() != 1 or starts.dim() != 1 or starts.shape[0] < 1:
         raise invalid("verify_drafts: target_probs must be [rows, vocab], drafts and starts lists")
     device = on_gpu(target_probs, draft_probs, drafts, starts, accept_u, sample_u)
+    if not is_current(device):
+        with torch.cuda.device(device):
+            return verify_drafts(target_probs, draft_probs, drafts, starts, max_drafts, accept_u,
+                                 sample_u)
     n, seqs, vocab = drafts.shape[0], starts.shape[0] - 1, target_probs.shape[1]
     if target_probs.shape[0] != n + seqs:
         raise invalid(f"{target_probs.shape[0]} target rows for {n} drafts of {seqs} sequences")
@@ -97,16 +108,15 @@ def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor
     sample_u = _array(sample_u, seqs, torch.float32, "sample_u")
     if max_drafts < 0:
         raise invalid(f"max_drafts {max_drafts}")
-    with at_device(device) as stream:
-        n_accepted = torch.empty(seqs, dtype=torch.int32, device=device)
-        tokens = torch.empty((seqs, max_drafts + 1), dtype=torch.int32, device=device)
-        size = S.stage_verify_bytes(seqs, vocab)
-        ws = torch.empty(size, dtype=torch.uint8, device=device)
-        # an empty draft_probs stays "given": no draft is there to ask
-        batch = S.stage_drafts(dt, vocab, seqs, n, max_drafts, p.data_ptr(), row_stride(p),
-                               None if q is None or n == 0 else q.data_ptr(),
-                               0 if q is None else row_stride(q), drafts.data_ptr(),
-                               starts.data_ptr(), accept_u.data_ptr(), sample_u.data_ptr())
-        S.stage_verify_drafts(batch, n_accepted.data_ptr(), tokens.data_ptr(), ws.data_ptr(), size,
-                              stream)
+    n_accepted = torch.empty(seqs, dtype=torch.int32, device=device)
+    tokens = torch.empty((seqs, max_drafts + 1), dtype=torch.int32, device=device)
+    size = _verify_bytes(seqs, vocab)
+    ws = scratch(size, device)
+    # an empty draft_probs is as good as none: there is no draft to ask it for
+    batch = S.stage_drafts(dt, vocab, seqs, n, max_drafts, p.data_ptr(), row_stride(p),
+                           None if q is None or n == 0 else q.data_ptr(),
+                           0 if q is None else row_stride(q), drafts.data_ptr(),
+                           starts.data_ptr(), accept_u.data_ptr(), sample_u.data_ptr())
+    S.stage_verify_drafts(batch, n_accepted.data_ptr(), tokens.data_ptr(), ws.data_ptr(), size,
+                          stream_of(device))
     return n_accepted, tokens

@@ -39,7 +39,7 @@ EXPORTED = ("stage_create", "stage_workspace_bytes", "stage_bind_workspace", "st
             "stage_decode_noalloc", "stage_store_alloc", "stage_store_free", "stage_store_write",
             "stage_store_attach", "stage_store_detach", "stage_quant_bytes", "stage_quant_rows",
             "stage_quant_pack", "stage_quant_product_bytes", "stage_quant_product",
-            "stage_lm_head_quant", "stage_token_probs_bytes", "stage_token_probs", "stage_verify_bytes",
+            "stage_quant_linear_bytes", "stage_quant_linear", "stage_lm_head_quant", "stage_token_probs_bytes", "stage_token_probs", "stage_verify_bytes",
             "stage_verify_drafts")
 
 STAGE_STORE_MAX_BYTES = 1 << 31
@@ -137,12 +137,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.stage_quant_pack.argtypes = [P, i64, P, i32, i32, P, P]
     lib.stage_quant_product_bytes.argtypes = [i32, i32, i32]
     lib.stage_quant_product.argtypes = [P, i32, P, i32, i32, i32, P, i64, P, size, P]
+    lib.stage_quant_linear_bytes.argtypes = [i32, i32, i32]
+    lib.stage_quant_linear.argtypes = [i32, P, i64, i32, i32, P, i32, i32, P, i64, P, size, P]
     lib.stage_lm_head_quant.argtypes = lib.stage_lm_head.argtypes
     lib.stage_token_probs_bytes.argtypes = [i32, i32]
     lib.stage_token_probs.argtypes = [i32, P, i64, i32, i32, P, i32, P, i64, P, size, P]
     lib.stage_verify_bytes.argtypes = [i32, i32]
     lib.stage_verify_drafts.argtypes = [ctypes.POINTER(stage_drafts), P, P, P, size, P]
-    for name in ("stage_quant_bytes", "stage_quant_product_bytes", "stage_token_probs_bytes", "stage_verify_bytes"):
+    for name in ("stage_quant_bytes", "stage_quant_product_bytes", "stage_quant_linear_bytes",
+                 "stage_token_probs_bytes", "stage_verify_bytes"):
         getattr(lib, name).restype = size
     lib.stage_set_op_timing.argtypes = [P, i32]
     lib.stage_read_op_times.argtypes = [P, ctypes.POINTER(ctypes.c_double),
@@ -154,7 +157,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                  "stage_copy_probe", "stage_lm_head", "stage_pack_lm_head", "stage_store_alloc",
                  "stage_store_free", "stage_store_write", "stage_store_attach",
                  "stage_store_detach", "stage_quant_rows", "stage_quant_pack",
-                 "stage_quant_product", "stage_lm_head_quant", "stage_token_probs",
+                 "stage_quant_product", "stage_quant_linear", "stage_lm_head_quant",
+                 "stage_token_probs",
                  "stage_verify_drafts"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -293,6 +297,17 @@ def stage_quant_product(a: int, m: int, b: int, n: int, k: int, out_dtype: int, 
                         ldo: int, ws: int, ws_bytes: int, stream: int = 0) -> None:
     _check(load_library().stage_quant_product(a, m, b, n, k, out_dtype, out, ldo, ws, ws_bytes,
                                               stream))
+
+
+def stage_quant_linear_bytes(m: int, n: int, k: int) -> int:
+    return load_library().stage_quant_linear_bytes(m, n, k)
+
+
+def stage_quant_linear(dtype: int, x: int, ld: int, m: int, k: int, w: int, n: int,
+                       out_dtype: int, out: int, ldo: int, ws: int, ws_bytes: int,
+                       stream: int = 0) -> None:
+    _check(load_library().stage_quant_linear(dtype, x, ld, m, k, w, n, out_dtype, out, ldo, ws,
+                                             ws_bytes, stream))
 
 
 def stage_token_probs_bytes(rows: int, vocab: int) -> int:

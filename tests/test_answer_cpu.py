@@ -73,6 +73,29 @@ def test_quant_product_refuses(args, code):
     _refused(_lib().stage_quant_product(*args, None, 0, None), code)
 
 
+@pytest.mark.parametrize("args,code", [
+    ((7, A, 64, 4, 64, B, 8, F32, C, 8), UNS), ((F32, A, 64, 4, 64, B, 8, 7, C, 8), UNS),
+    ((F32, A, 64, -4, 64, B, 8, F32, C, 8), INV), ((F32, A, 64, 4, 64, B, -8, F32, C, 8), INV),
+    ((F32, A, 64, 4, 0, B, 8, F32, C, 8), INV), ((F32, A, 63, 4, 64, B, 8, F32, C, 8), INV),
+    ((F32, 0, 64, 4, 64, B, 8, F32, C, 8), INV), ((F32, A + 2, 64, 4, 64, B, 8, F32, C, 8), INV),
+    ((F32, A, 64, 4, 64, 0, 8, F32, C, 8), INV), ((F32, A, 64, 4, 64, B + 8, 8, F32, C, 8), INV),
+    ((F32, A, 64, 4, 64, B, 8, F32, 0, 8), INV), ((F32, A, 64, 4, 64, B, 8, F32, C, 7), INV),
+    ((F32, A, 1 << 18, 4, 131073, B, 8, F32, C, 8), UNS),
+])
+def test_quant_linear_refuses(args, code):
+    _refused(_lib().stage_quant_linear(*args, D, 1 << 20, None), code)
+
+
+def test_quant_linear_checks_its_workspace():
+    lib = _lib()
+    need = S.stage_quant_linear_bytes(128, 1280, 8192)
+    assert need >= S.stage_quant_bytes(128, 8192) + S.stage_quant_product_bytes(128, 1280, 8192)
+    assert S.stage_quant_linear_bytes(4, 0, 64) == 0 == S.stage_quant_linear_bytes(4, 8, -1)
+    for ws, size, code in ((0, need, INV), (D, need - 1, CAP), (D + 8, need, INV)):
+        _refused(lib.stage_quant_linear(F32, A, 8192, 128, 8192, B, 1280, F32, C, 1280, ws, size,
+                                        None), code)
+
+
 def test_empty_calls_do_nothing():
     lib = _lib()
     assert lib.stage_quant_rows(F32, None, 0, 0, 64, None, None) == S.STAGE_OK
@@ -81,6 +104,8 @@ def test_empty_calls_do_nothing():
                                    None) == S.STAGE_OK
     assert lib.stage_quant_product(None, 8, None, 0, 64, F32, None, 0, None, 0,
                                    None) == S.STAGE_OK
+    assert lib.stage_quant_linear(F32, None, 64, 0, 64, None, 8, F32, None, 8, None, 0,
+                                  None) == S.STAGE_OK
     assert lib.stage_token_probs(F32, None, 0, 0, 64, None, F32, None, 0, None, 0,
                                  None) == S.STAGE_OK
     empty = S.stage_drafts(F32, 64, 0, 0, 4)
