@@ -111,12 +111,12 @@ def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor
     n_accepted = torch.empty(seqs, dtype=torch.int32, device=device)
     tokens = torch.empty((seqs, max_drafts + 1), dtype=torch.int32, device=device)
     size = _verify_bytes(seqs, vocab)
-    ws = scratch(size, device)
+    ws = scratch(size, device).data_ptr() if size else None
     # an empty draft_probs is as good as none: there is no draft to ask it for
     batch = S.stage_drafts(dt, vocab, seqs, n, max_drafts, p.data_ptr(), row_stride(p),
                            None if q is None or n == 0 else q.data_ptr(),
                            0 if q is None else row_stride(q), drafts.data_ptr(),
                            starts.data_ptr(), accept_u.data_ptr(), sample_u.data_ptr())
-    S.stage_verify_drafts(batch, n_accepted.data_ptr(), tokens.data_ptr(), ws.data_ptr(), size,
+    S.stage_verify_drafts(batch, n_accepted.data_ptr(), tokens.data_ptr(), ws, size,
                           stream_of(device))
     return n_accepted, tokens
