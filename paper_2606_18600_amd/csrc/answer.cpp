@@ -40,8 +40,6 @@ bool at_multiple(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 size_t esize(int d) { return d == STAGE_F32 ? 4 : 2; }
 
-size_t align16(size_t n) { return (n + 15) / 16 * 16; }
-
 // A quantised matrix's size, as every call checks it.
 stage_status check_matrix(int32_t rows, int32_t k, const char* what) {
   if (rows < 0 || k < 1)
@@ -137,7 +135,7 @@ stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_
 size_t stage_quant_linear_bytes(int32_t m, int32_t n, int32_t k) {
   if (m < 1 || n < 1 || check_matrix(m, k, "x") != STAGE_OK || check_matrix(n, k, "w") != STAGE_OK)
     return 0;
-  return align16(quant_bytes(m, k)) + quant_plane_bytes(quant_plan(m, n, k, SIZE_MAX), m, n);
+  return quant_linear_bytes(quant_plan(m, n, k, SIZE_MAX, true), m, n, k);
 }
 
 stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, int32_t m, int32_t k,
@@ -153,14 +151,10 @@ stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, in
   if ((v = check_rows(x, ld, k, esize(d), "x")) != STAGE_OK) return v;
   if ((v = check_packed(w, "w")) != STAGE_OK) return v;
   if ((v = check_rows(out, ldo, n, esize(o), "out")) != STAGE_OK) return v;
-  const QuantPlan plan = quant_plan(m, n, k, SIZE_MAX);
-  const size_t planes = align16(quant_bytes(m, k));
-  if ((v = check_workspace(ws, ws_bytes, planes + quant_plane_bytes(plan, m, n))) != STAGE_OK)
-    return v;
-  hipStream_t s = (hipStream_t)stream;
-  if ((v = launched("quant_rows", quant_rows((DType)d, x, ld, m, k, ws, s))) != STAGE_OK) return v;
-  return launched("quant_product", quant_product(plan, ws, m, w, n, k, (DType)o, out, ldo,
-                                                 (char*)ws + planes, s));
+  const QuantPlan plan = quant_plan(m, n, k, SIZE_MAX, true);
+  if ((v = check_workspace(ws, ws_bytes, quant_linear_bytes(plan, m, n, k))) != STAGE_OK) return v;
+  return launched("quant_linear", quant_linear(plan, (DType)d, x, ld, m, w, n, k, (DType)o, out,
+                                               ldo, ws, (hipStream_t)stream));
 }
 
 stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void* w_lm,

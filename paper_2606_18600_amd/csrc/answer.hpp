@@ -58,17 +58,30 @@ constexpr int kSkinnyStrips = 12;  // ... and the skinny kernel
 constexpr int quant_skinny_strips(int strips) { return strips <= 1 ? 1 : (strips + 1) / 2 * 2; }
 // A product's kernel and its k ranges of kt_len k tiles of 64. Several ranges
 // leave an int32 plane [M][N rounded up to 16] each, which a last kernel adds.
+// fused: the stream kernel quantises the rows itself (quant_linear).
 struct QuantPlan {
   QuantKernel kernel = QUANT_TILE_4X4;
   int ranges = 1, kt_len = 0;
+  bool fused = false;
 };
-// The plan of a product whose planes may take `room` bytes.
-QuantPlan quant_plan(int M, int N, int K, size_t room);
+constexpr int kFusedRows = 4;
+// The plan of a product whose planes may take `room` bytes; with `rows`, of rows
+// that are still to be quantised.
+QuantPlan quant_plan(int M, int N, int K, size_t room, bool rows = false);
 size_t quant_plane_bytes(const QuantPlan& p, int M, int N);
 // out [M, N] (fp32 or bf16, row stride ldo) = a b^T for the 8-bit matrices a
 // [M, K] and b [N, K]; planes: quant_plane_bytes() bytes.
 hipError_t quant_product(const QuantPlan& p, const void* a, int M, const void* b, int N, int K,
                          DType out_dt, void* out, int64_t ldo, void* planes, hipStream_t s);
+// ... of rows x [M, K] (fp32 or bf16, row stride ld) that are quantised on the way.
+// ws: quant_linear_bytes().
+inline size_t quant_planes_at(int M, int K) { return (quant_bytes(M, K) + 15) / 16 * 16; }
+inline size_t quant_linear_bytes(const QuantPlan& p, int M, int N, int K) {
+  return p.fused ? 0 : quant_planes_at(M, K) + quant_plane_bytes(p, M, N);
+}
+hipError_t quant_linear(const QuantPlan& p, DType dt, const void* x, int64_t ld, int M,
+                        const void* b, int N, int K, DType out_dt, void* out, int64_t ldo,
+                        void* ws, hipStream_t s);
 
 // probs[r] = softmax(logits[r] / temperature[r]) (temperature: device [rows],
 // nullptr for 1). ws: token_probs_bytes().

@@ -57,15 +57,16 @@ size_t quant_plane_bytes(const QuantPlan& p, int M, int N) {
   return p.ranges > 1 ? (size_t)p.ranges * M * quant_rows16(N) * 4 : 0;
 }
 
-QuantPlan quant_plan(int M, int N, int K, size_t room) {
+QuantPlan quant_plan(int M, int N, int K, size_t room, bool unquantised) {
   const long strips = up(N, 16), tiles = up(M, 16), KT = (long)quant_kp(K) / 64;
   const double mb = ((double)N * K + (double)M * K + (double)M * N * 2) * 1e-6;
   const double weights = (double)N * K;
   QuantPlan best;
   double least = 1e30;
-  auto offer = [&](QuantKernel kind, long kt_len, double us) {
+  auto offer = [&](QuantKernel kind, long kt_len, double us, bool fused = false) {
     QuantPlan p;
     p.kernel = kind;
+    p.fused = fused;
     p.kt_len = (int)kt_len;
     p.ranges = (int)up(KT, kt_len);
     if (p.ranges > 1) {
@@ -78,8 +79,13 @@ QuantPlan quant_plan(int M, int N, int K, size_t room) {
   if (tiles <= kStreamStrips)
     for (int nf : {1, 3}) {
       const long rounds = up(up(strips, nf), kCus);
+      // a launch for the rows' 8-bit values costs 4 us (1 x 8192 x 28672: 43.6 us
+      // with it, V_FUSED without)
+      const bool fused = unquantised && M <= kFusedRows;
       offer(nf == 1 ? QUANT_STREAM_1 : QUANT_STREAM_3, KT,
-            std::max(mb / 6.6, rounds * KT * (M / 16.0 + nf) / 48.5) + 0.28 * rounds);
+            std::max(mb / 6.6, rounds * KT * (M / 16.0 + nf) / 48.5) + 0.28 * rounds -
+                (fused ? 4.0 : 0.0),
+            fused);
     }
   if (tiles <= kSkinnyStrips) {
     const long mt = quant_skinny_strips((int)tiles);

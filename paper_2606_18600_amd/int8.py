@@ -195,7 +195,7 @@ def linear(x: torch.Tensor, w: Matrix, dtype: Optional[torch.dtype] = None) -> t
     m = x.shape[0]
     y = torch.empty((m, n), dtype=dtype, device=device)
     size = _linear_bytes(m, n, k)
-    ws = scratch(size, device)
+    ws = scratch(size, device).data_ptr() if size else None
     S.stage_quant_linear(dt, x.data_ptr(), row_stride(x), m, k, w.data.data_ptr(), n, dt_out,
-                         y.data_ptr(), n, ws.data_ptr(), size, stream_of(device))
+                         y.data_ptr(), n, ws, size, stream_of(device))
     return y if len(shape) == 2 else y.view(*shape[:-1], n)
