@@ -38,10 +38,11 @@ hipError_t quant_norm_rows(DType dt, const void* src, const int32_t* idx, const 
                            float eps, int rows, int K, void* dst, hipStream_t s);
 
 // The kernels of a product (k_quant.hip): operands streamed into registers by
-// blocks of 1 or 3 strips of 16 columns; the skinny kernel with NF strips for each
+// blocks of 1 to 3 strips of 16 columns; the skinny kernel with NF strips for each
 // of WC groups of waves; tiles of BM x BN strips.
 enum QuantKernel {
   QUANT_STREAM_1,
+  QUANT_STREAM_2,  // (rows quantised on the way only)
   QUANT_STREAM_3,
   QUANT_SKINNY_2X2,
   QUANT_SKINNY_4X2,

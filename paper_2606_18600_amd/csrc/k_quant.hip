@@ -774,6 +774,8 @@ hipError_t launch_linear(const XT* x, int64_t ld, int K, const Product& p, OutT*
                          int64_t ldo) {
   if (p.plan.kernel == QUANT_STREAM_1)
     launch_fused<1>(x, ld, K, p, out, ldo);
+  else if (p.plan.kernel == QUANT_STREAM_2)
+    launch_fused<2>(x, ld, K, p, out, ldo);
   else
     launch_fused<3>(x, ld, K, p, out, ldo);
   return hipGetLastError();

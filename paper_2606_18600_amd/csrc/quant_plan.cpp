@@ -49,6 +49,7 @@ constexpr Skinny kSkinny[] = {{QUANT_SKINNY_2X2, 2, 2},
                               {QUANT_SKINNY_4X2, 4, 2},
                               {QUANT_SKINNY_4X4, 4, 4},
                               {QUANT_SKINNY_4X8, 4, 8}};
+constexpr QuantKernel kStream[] = {QUANT_STREAM_1, QUANT_STREAM_2, QUANT_STREAM_3};
 constexpr int kRanges[] = {1, 2, 3, 4, 6, 8};
 
 }  // namespace
@@ -76,16 +77,23 @@ QuantPlan quant_plan(int M, int N, int K, size_t room, bool unquantised) {
     }
     if (us < least) least = us, best = p;
   };
+  if (unquantised && M <= kFusedRows) {
+    // One launch that quantises the rows on the way, against 4 us for a launch of
+    // its own (1 x 8192 x 28672 on 1, 2, 3 strips a block: 48.1, 39.6, 41.9 us in all;
+    // 1 x 8192 x 8192 17.5, 16.3, 15.1; 1 x 1280 x 8192 10.5, 11.5, 12.9).
+    for (int nf : {1, 2, 3}) {
+      const long blocks = up(strips, nf), rounds = up(blocks, kCus);
+      offer(kStream[nf - 1], KT,
+            std::max(mb / 6.6, rounds * KT * nf / 34.0) + 0.28 * rounds +
+                0.014 * std::min<long>(blocks, kCus) - 4.0,
+            true);
+    }
+  }
   if (tiles <= kStreamStrips)
     for (int nf : {1, 3}) {
       const long rounds = up(up(strips, nf), kCus);
-      // a launch for the rows' 8-bit values costs 4 us (1 x 8192 x 28672: 43.6 us
-      // with it, V_FUSED without)
-      const bool fused = unquantised && M <= kFusedRows;
-      offer(nf == 1 ? QUANT_STREAM_1 : QUANT_STREAM_3, KT,
-            std::max(mb / 6.6, rounds * KT * (M / 16.0 + nf) / 48.5) + 0.28 * rounds -
-                (fused ? 4.0 : 0.0),
-            fused);
+      offer(kStream[nf - 1], KT,
+            std::max(mb / 6.6, rounds * KT * (M / 16.0 + nf) / 48.5) + 0.28 * rounds);
     }
   if (tiles <= kSkinnyStrips) {
     const long mt = quant_skinny_strips((int)tiles);

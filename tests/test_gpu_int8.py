@@ -107,6 +107,23 @@ def test_linear_many_columns(m, n, k):
     _close(y[:, cols], _reference(x, w[cols]), "f32")
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 8190, 28671), (2, 5, 3), (3, 57339, 8191), (4, 10239, 5119),
+                                   (4, 1279, 8190), (1, 16, 16), (3, 4100, 64), (4, 700, 100)])
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f32", "f32"), ("bf16", "bf16"),
+                                       ("f32", "bf16")])
+def test_few_rows_are_quantised_on_the_way(m, n, k, dtype, out):
+    """Up to four rows, in one launch: the same values as with quantised rows, also
+    from rows with a gap between them, and rows of NaN and zeros beside others."""
+    wide = _draw(m + 5, m, k + 9, dtype)
+    x, w = wide[:, 3:3 + k], int8.quantize(_draw(n, n, k, "bf16"))
+    y = int8.linear(x, w, TD[out])
+    assert torch.equal(y, int8.product(int8.quantize(x), w, TD[out]))
+    if m > 1:
+        x[0, k // 2], x[1] = float("nan"), 0
+        z = int8.linear(x, w, TD[out])
+        assert z[0].isnan().all() and (z[1] == 0).all() and torch.equal(z[2:], y[2:])
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 40, 200), (70, 100, 384), (300, 520, 256), (1030, 64, 130)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_and_addresses(m, n, k, dtype):
