@@ -16,21 +16,20 @@ typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
 template <typename T> struct vec16;
 template <> struct vec16<float> {
   static constexpr int kN = 4;
-  __device__ static __forceinline__ void load(const float* p, float (&v)[4]) {
-    const f32x4_any_t w = *(const f32x4_any_t*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = w[e];
-  }
+  f32x4_t w;
+  __device__ __forceinline__ void load(const float* p) { w = *(const f32x4_any_t*)p; }
+  __device__ __forceinline__ void set(int e, float v) { w[e] = v; }
+  __device__ __forceinline__ float get(int e) const { return w[e]; }
 };
 template <> struct vec16<bf16_t> {
   static constexpr int kN = 8;
-  __device__ static __forceinline__ void load(const bf16_t* p, float (&v)[8]) {
-    const u32x4_any_t w = *(const u32x4_any_t*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[2 * e] = lo_bf16(w[e]);
-      v[2 * e + 1] = hi_bf16(w[e]);
-    }
+  u32x4_t w;
+  __device__ __forceinline__ void load(const bf16_t* p) { w = *(const u32x4_any_t*)p; }
+  __device__ __forceinline__ void set(int e, bf16_t v) {
+    w[e / 2] = e % 2 ? (w[e / 2] & 0xffffu) | (uint32_t)v << 16 : (w[e / 2] & 0xffff0000u) | v;
+  }
+  __device__ __forceinline__ float get(int e) const {
+    return e % 2 ? hi_bf16(w[e / 2]) : lo_bf16(w[e / 2]);
   }
 };
 
@@ -42,16 +41,25 @@ template <int V, bool kShort>
 __device__ __forceinline__ int vec_at(int k, int n) {
   return kShort ? k : min(k, n - V);
 }
-// Reads it: v[e] is value vec_at() + e.
+// Reads it, as it lies in memory: value e is value vec_at() + e of the row.
+template <bool kShort, typename T>
+__device__ __forceinline__ void read_vec(const T* row, int k, int n, vec16<T>& v) {
+  constexpr int V = vec16<T>::kN;
+  if constexpr (kShort) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.set(e, k + e < n ? row[k + e] : (T)0);
+  } else {
+    v.load(row + vec_at<V, kShort>(k, n));
+  }
+}
+// ... as floats.
 template <int V, bool kShort, typename T>
 __device__ __forceinline__ void load_vec(const T* row, int k, int n, float (&v)[V]) {
   static_assert(V == vec16<T>::kN, "16 bytes");
-  if constexpr (kShort) {
+  vec16<T> w;
+  read_vec<kShort>(row, k, n, w);
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = k + e < n ? elem<T>::load(row, k + e) : 0.f;
-  } else {
-    vec16<T>::load(row + vec_at<V, kShort>(k, n), v);
-  }
+  for (int e = 0; e < V; ++e) v[e] = w.get(e);
 }
 // Puts `fill` where a value is another vector's (below k) or the row ends before k.
 template <int V, bool kShort>
@@ -310,23 +318,23 @@ hipError_t launch_probs(const T* x, int64_t ld, int rows, int vocab, const float
 // fall within 1e-15 of a draw. Weights that are not positive and finite count
 // as 0.
 //
-// Bound: HBM, one target row and at most one draft row per sequence. The sums
-// of kBlockVals values at a time (a wave each) go to the workspace, a second
-// kernel finds the block and then the token in it.
+// Bound: HBM, one target row and at most one draft row per sequence, and for a few
+// sequences on a CU each its fp64 adds. The sums of kBlockVals weights at a time (a
+// wave each) tell the block, a scan in it the token.
 constexpr int kBlockVals = 1024;
 constexpr int kLaneVals = kBlockVals / 64;
 constexpr int kRowBlocks = 1024;  // blocks whose sums fit a block's LDS
 
+// Where a sequence's weights come from: its target row; that row without the refused
+// token, which was chosen outright; what the draft's row leaves of it.
+enum Weights { kRow, kRowBut, kRest };
+
 struct Stop {
   int n;         // accepted drafts
   int s0;        // the sequence's first draft
-  bool refused;  // draft n was refused
-  int token;     // ... which was this one
+  int token;     // the refused draft
+  Weights kind;  // kRow: none was refused
 };
-
-__device__ __forceinline__ double weight(float w) {
-  return w > 0.f && w < INFINITY ? (double)w : 0.0;
-}
 
 // Every lane of a wave gets the same answer. Offsets and tokens outside their
 // ranges read nothing: the ranges are clamped, such a token is refused.
@@ -340,8 +348,8 @@ __device__ __forceinline__ Stop first_refusal(const VerifyArgs& a, int seq) {
   const int s1 = min(max(a.starts[seq + 1], st.s0), a.n_drafts);
   const int count = min(s1 - st.s0, a.most);
   st.n = count;
-  st.refused = false;
   st.token = -1;
+  st.kind = kRow;
   for (int j0 = 0; j0 < count; j0 += 64) {
     const int j = j0 + lane;
     bool no = false;
@@ -361,53 +369,13 @@ __device__ __forceinline__ Stop first_refusal(const VerifyArgs& a, int seq) {
     if (mask) {
       const int l = __ffsll(mask) - 1;
       st.n = j0 + l;
-      st.refused = true;
       st.token = __shfl(d, l, 64);
+      st.kind = q ? kRest : kRowBut;
       break;
     }
   }
   return st;
 }
-
-// Vectors j < NV of the target's row that the new token comes from, the j-th at token
-// t0 + j kStep, and (kDraft) of the draft's row; zeros past the end.
-template <int NV, int kStep, int V, bool kShort, bool kDraft, typename T>
-__device__ __forceinline__ void load_weights(const VerifyArgs& a, const Stop& st, int seq, int t0,
-                                             float (&p)[NV][V], float (&q)[NV][V]) {
-  const T* pr = (const T*)a.target + (int64_t)(st.s0 + seq + st.n) * a.ld_target;
-  const T* qr = (const T*)a.draft + (kDraft ? (int64_t)(st.s0 + st.n) * a.ld_draft : 0);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    load_vec<V, kShort>(pr, t0 + j * kStep, a.vocab, p[j]);
-    if constexpr (kDraft) load_vec<V, kShort>(qr, t0 + j * kStep, a.vocab, q[j]);
-  }
-#pragma unroll
-  for (int j = 0; j < NV; ++j)  // (what is left of no weight is nothing, whatever q is)
-    trim_vec<V, kShort>(t0 + j * kStep, a.vocab, 0.f, p[j]);
-  if constexpr (!kDraft)
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int e = 0; e < V; ++e) q[j][e] = 0.f;
-}
-
-// What is left of token t's weight x: the draft's probability q is taken off (all
-// of it where the refused draft was chosen outright).
-__device__ __forceinline__ double left_of(const VerifyArgs& a, const Stop& st, int t, double x,
-                                          float q) {
-  const double d = x - (double)q;
-  return d > 0.0 && !(st.refused && !a.draft && t == st.token) ? d : 0.0;
-}
-
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
-struct BlockSum {
-  double left, all;
-};
 
 // The accepted drafts and what follows the new token's place.
 __device__ __forceinline__ void write_accepted(const VerifyArgs& a, const Stop& st, int seq,
@@ -418,39 +386,110 @@ __device__ __forceinline__ void write_accepted(const VerifyArgs& a, const Stop& 
       a.tokens[(size_t)seq * (a.most + 1) + j] = j < st.n ? a.drafts[st.s0 + j] : -1;
 }
 
+template <int kKind>
+__device__ __forceinline__ double weight_of(float p, float q, int t, int refused) {
+  if (kKind == kRest) {
+    const double d = (double)p - (double)q;
+    return d > 0.0 && d < (double)INFINITY ? d : 0.0;
+  }
+  return p > 0.f && p < INFINITY && !(kKind == kRowBut && t == refused) ? (double)p : 0.0;
+}
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// NV vectors of a sequence's target row and (kRest) draft row.
+template <typename T, int kKind, int NV> struct RowVals {
+  vec16<T> p[NV], q[kKind == kRest ? NV : 1];
+  __device__ __forceinline__ float draft(int j, int e) const {
+    return kKind == kRest ? q[kKind == kRest ? j : 0].get(e) : 0.f;
+  }
+};
+template <typename T, int kKind> struct RowPtr {
+  const T *p, *q;
+  __device__ __forceinline__ RowPtr(const VerifyArgs& a, const Stop& st, int seq)
+      : p((const T*)a.target + (int64_t)(st.s0 + seq + st.n) * a.ld_target),
+        q(kKind == kRest ? (const T*)a.draft + (int64_t)(st.s0 + st.n) * a.ld_draft : nullptr) {}
+  template <bool kShort, int NV>
+  __device__ __forceinline__ void read(RowVals<T, kKind, NV>& v, int j, int t, int vocab) const {
+    read_vec<kShort>(p, t, vocab, v.p[j]);
+    if constexpr (kKind == kRest) read_vec<kShort>(q, t, vocab, v.q[j]);
+  }
+};
+
 // The sums of the weights of blocks b, b + step, ... (kBlockVals tokens each) of a
-// sequence, by one wave.
-template <typename T, bool kShort, bool kDraft>
+// sequence, by one wave; a block is read while the one before it is summed.
+template <typename T, bool kShort, int kKind>
 __device__ __forceinline__ void block_sums(const VerifyArgs& a, const Stop& st, int seq, int b,
-                                           int blocks, int step, BlockSum* sums) {
+                                           int blocks, int step, double* sums) {
   constexpr int V = vec16<T>::kN, NV = kLaneVals / V;
-  for (; b < blocks; b += step) {
-    const int t0 = b * kBlockVals + (threadIdx.x & 63) * V;
-    float p[NV][V], q[NV][V];
-    load_weights<NV, V * 64, V, kShort, kDraft, T>(a, st, seq, t0, p, q);
-    double l = 0.0, w = 0.0;
+  typedef RowVals<T, kKind, NV> Vals;
+  const int lane = threadIdx.x & 63;
+  const RowPtr<T, kKind> row(a, st, seq);
+  auto token = [&](int blk, int j) { return blk * kBlockVals + (j * 64 + lane) * V; };
+  auto read = [&](Vals& v, int blk) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) row.template read<kShort>(v, j, token(blk, j), a.vocab);
+  };
+  auto sum = [&](const Vals& v, int blk) {
+    double l = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int at = vec_at<V, kShort>(t0 + j * V * 64, a.vocab);
+      const int k = token(blk, j), at = vec_at<V, kShort>(k, a.vocab);
+      float p[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) p[e] = v.p[j].get(e);
+      trim_vec<V, kShort>(k, a.vocab, 0.f, p);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const double x = weight(p[j][e]);
-        w += x;
-        l += left_of(a, st, at + e, x, q[j][e]);
+        // a maximum with 0 drops what is negative or NaN
+        if (kKind == kRest)
+          l += fmax((double)p[e] - (double)v.draft(j, e), 0.0);
+        else
+          l += (double)fmaxf(kKind == kRowBut && at + e == st.token ? 0.f : p[e], 0.f);
       }
     }
     l = wave_sum64(l);
-    w = wave_sum64(w);
-    if ((threadIdx.x & 63) == 0) sums[b] = BlockSum{l, w};
+    if (!(l < (double)INFINITY)) {  // an infinity among them: without it
+      l = 0.0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int k = token(blk, j), at = vec_at<V, kShort>(k, a.vocab);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (kShort ? k + e < a.vocab : at + e >= k)
+            l += weight_of<kKind>(v.p[j].get(e), v.draft(j, e), at + e, st.token);
+      }
+      l = wave_sum64(l);
+    }
+    if (lane == 0) sums[blk] = l;
+  };
+  Vals even, odd;
+  if (b < blocks) read(even, b);
+  while (b < blocks) {
+    const int next = b + step, after = next + step;
+    if (next < blocks) read(odd, next);
+    __builtin_amdgcn_sched_barrier(0);
+    sum(even, b);
+    if (next >= blocks) break;
+    if (after < blocks) read(even, after);
+    __builtin_amdgcn_sched_barrier(0);
+    sum(odd, next);
+    b = after;
   }
 }
 template <typename T, bool kShort>
 __device__ __forceinline__ void block_sums(const VerifyArgs& a, const Stop& st, int seq, int b,
-                                           int blocks, int step, BlockSum* sums) {
-  if (st.refused && a.draft)
-    block_sums<T, kShort, true>(a, st, seq, b, blocks, step, sums);
+                                           int blocks, int step, double* sums) {
+  if (st.kind == kRest)
+    block_sums<T, kShort, kRest>(a, st, seq, b, blocks, step, sums);
+  else if (st.kind == kRowBut)
+    block_sums<T, kShort, kRowBut>(a, st, seq, b, blocks, step, sums);
   else
-    block_sums<T, kShort, false>(a, st, seq, b, blocks, step, sums);
+    block_sums<T, kShort, kRow>(a, st, seq, b, blocks, step, sums);
 }
 
 // Exclusive prefix of v over the wave's lanes, and the total.
@@ -477,73 +516,102 @@ __device__ __forceinline__ int find_lane(double prefix, double v, double want) {
   return some ? 63 - __clzll(some) : -1;
 }
 
-// The token that the random number names, by one wave: first among the blocks' sums,
-// then in the block.
+// The token in a block whose weights before it sum to `before`, by one wave.
+template <typename T, bool kShort, int kKind>
+__device__ __forceinline__ int pick_in_block(const VerifyArgs& a, const Stop& st, int seq, int block,
+                                             double before, double want) {
+  constexpr int V = vec16<T>::kN, NV = kLaneVals / V;
+  const int t0 = block * kBlockVals + (threadIdx.x & 63) * kLaneVals;
+  const RowPtr<T, kKind> row(a, st, seq);
+  RowVals<T, kKind, NV> v;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) row.template read<kShort>(v, j, t0 + j * V, a.vocab);
+  double x[NV][V], mine = 0.0, sum;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int k = t0 + j * V, at = vec_at<V, kShort>(k, a.vocab);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const bool in = kShort ? k + e < a.vocab : at + e >= k;
+      x[j][e] = in ? weight_of<kKind>(v.p[j].get(e), v.draft(j, e), at + e, st.token) : 0.0;
+      mine += x[j][e];
+    }
+  }
+  double run = before + wave_prefix(mine, sum);
+  const int hit = find_lane(run, mine, want);
+  int pick = -1;
+  bool done = false;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = vec_at<V, kShort>(t0 + j * V, a.vocab);
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (x[j][e] > 0.0 && !done) {
+        pick = at + e;
+        run += x[j][e];
+        done = run > want;
+      }
+  }
+  return __shfl(pick, hit, 64);
+}
+
+// The token that the random number names, or -1 where no weight is positive, by one
+// wave: first among the blocks' sums, then in the block.
 template <typename T, bool kShort>
 __device__ __forceinline__ int pick_token(const VerifyArgs& a, const Stop& st, int seq, int blocks,
-                                          const BlockSum* bs) {
+                                          const double* sums) {
   const int lane = threadIdx.x & 63;
   const int per = (blocks + 63) / 64, b0 = min(lane * per, blocks), b1 = min(b0 + per, blocks);
-  double l = 0.0, w = 0.0, total;
-  for (int b = b0; b < b1; ++b) l += bs[b].left, w += bs[b].all;
-  double lt, wt;
-  const double lp = wave_prefix(l, lt), wp = wave_prefix(w, wt);
-  const bool use_left = lt > 0.0;
-  total = use_left ? lt : wt;
-  int token = -1;
-  if (total > 0.0) {
-    const double want = (double)a.sample_u[seq] * total;
-    double run = use_left ? lp : wp;
-    const double v = use_left ? l : w;
-    const int src = find_lane(run, v, want);
-    int pick = -1;
-    double before = run;
-    for (int b = b0; b < b1; ++b) {
-      const double x = use_left ? bs[b].left : bs[b].all;
-      if (x > 0.0) pick = b, before = run;
-      run += x;
-      if (x > 0.0 && run > want) break;
-    }
-    const int block = __shfl(pick, src, 64);
-    before = __shfl(before, src, 64);
-    constexpr int V = vec16<T>::kN, NV = kLaneVals / V;
-    const int t0 = block * kBlockVals + lane * kLaneVals;
-    float p[NV][V], q[NV][V];
-    double x[NV][V], mine = 0.0, sum;
-    if (st.refused && a.draft)
-      load_weights<NV, V, V, kShort, true, T>(a, st, seq, t0, p, q);
-    else
-      load_weights<NV, V, V, kShort, false, T>(a, st, seq, t0, p, q);
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        x[j][e] = weight(p[j][e]);
-        const int t = vec_at<V, kShort>(t0 + j * V, a.vocab) + e;
-        if (use_left) x[j][e] = left_of(a, st, t, x[j][e], q[j][e]);
-        mine += x[j][e];
-      }
-    run = before + wave_prefix(mine, sum);
-    const int hit = find_lane(run, mine, want);
-    pick = -1;
-    bool done = false;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (x[j][e] > 0.0 && !done) {
-          pick = vec_at<V, kShort>(t0 + j * V, a.vocab) + e;
-          run += x[j][e];
-          done = run > want;
-        }
-    token = __shfl(pick, hit, 64);
+  double mine = 0.0, total;
+  for (int b = b0; b < b1; ++b) mine += sums[b];
+  double run = wave_prefix(mine, total);
+  if (!(total > 0.0)) return -1;
+  const double want = (double)a.sample_u[seq] * total;
+  const int src = find_lane(run, mine, want);
+  int block = -1;
+  double before = run;
+  for (int b = b0; b < b1; ++b) {
+    const double x = sums[b];
+    if (x > 0.0) block = b, before = run;
+    run += x;
+    if (x > 0.0 && run > want) break;
   }
-  return token;
+  block = __shfl(block, src, 64);
+  before = __shfl(before, src, 64);
+  if (st.kind == kRest) return pick_in_block<T, kShort, kRest>(a, st, seq, block, before, want);
+  if (st.kind == kRowBut) return pick_in_block<T, kShort, kRowBut>(a, st, seq, block, before, want);
+  return pick_in_block<T, kShort, kRow>(a, st, seq, block, before, want);
+}
+
+// The whole block: writes a sequence's new token, given its blocks' sums. Where
+// nothing is left of a refused position's weights, its target row takes their place.
+template <typename T, bool kShort, int THREADS>
+__device__ __forceinline__ void draw_token(const VerifyArgs& a, Stop st, int seq, int blocks,
+                                           double* sums) {
+  __shared__ int drawn;
+  const int wave = threadIdx.x >> 6;
+  int* to = a.tokens + (size_t)seq * (a.most + 1) + st.n;
+  if (wave == 0) {
+    const int token = pick_token<T, kShort>(a, st, seq, blocks, sums);
+    if (threadIdx.x == 0) {
+      drawn = token;
+      *to = token;
+    }
+  }
+  if (st.kind == kRow) return;
+  __syncthreads();
+  if (drawn >= 0) return;
+  st.kind = kRow;
+  block_sums<T, kShort, kRow>(a, st, seq, wave, blocks, THREADS / 64, sums);
+  __syncthreads();
+  if (wave == 0) {
+    const int token = pick_token<T, kShort>(a, st, seq, blocks, sums);
+    if (threadIdx.x == 0) *to = token;
+  }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a,
-                                                          BlockSum* __restrict__ sums) {
+__global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, double* __restrict__ sums) {
   const int seq = blockIdx.y, wave = threadIdx.x >> 6;
   const int blocks = (a.vocab + kBlockVals - 1) / kBlockVals;
   const Stop st = first_refusal<T>(a, seq);
@@ -553,39 +621,36 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a,
 }
 
 template <typename T>
-__global__ __launch_bounds__(64) void verify_pick_kernel(VerifyArgs a,
-                                                         const BlockSum* __restrict__ sums) {
+__global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a, double* sums) {
   const int seq = blockIdx.x, blocks = (a.vocab + kBlockVals - 1) / kBlockVals;
-  const Stop st = first_refusal<T>(a, seq);
-  const int token = pick_token<T, false>(a, st, seq, blocks, sums + (size_t)seq * blocks);
-  if (threadIdx.x == 0) a.tokens[(size_t)seq * (a.most + 1) + st.n] = token;
+  draw_token<T, false, 256>(a, first_refusal<T>(a, seq), seq, blocks,
+                            sums + (size_t)seq * blocks);
 }
 
 // A whole sequence by one block of 16 waves, the sums in LDS.
 template <typename T, bool kShort>
 __global__ __launch_bounds__(1024) void verify_row_kernel(VerifyArgs a) {
-  __shared__ BlockSum sums[kRowBlocks];
+  __shared__ double sums[kRowBlocks];
   const int seq = blockIdx.x, wave = threadIdx.x >> 6;
   const int blocks = (a.vocab + kBlockVals - 1) / kBlockVals;
   const Stop st = first_refusal<T>(a, seq);
   write_accepted(a, st, seq, 1024);
   block_sums<T, kShort>(a, st, seq, wave, blocks, 16, sums);
   __syncthreads();
-  if (wave != 0) return;
-  const int token = pick_token<T, kShort>(a, st, seq, blocks, sums);
-  if (threadIdx.x == 0) a.tokens[(size_t)seq * (a.most + 1) + st.n] = token;
+  draw_token<T, kShort, 1024>(a, st, seq, blocks, sums);
 }
 
 // One block per sequence where there are enough of them (256 of 128256 tokens in
-// fp32: 40.2 us, against 37.8 + 5.4 in two launches; 64: 23.8 against 9.5 + 5.1) or
-// where its 16 waves have two blocks of tokens each at most.
+// fp32: 48.9 us, against 52.5 in two launches; 128: 30.7 against 25.5, one: 14.5
+// against 7.3) or where its 16 waves have four blocks of tokens each at most (50000
+// tokens, one sequence: 8.0 against 6.8 and a launch; 64: 11.0 against 11.5).
 bool verify_by_rows(int seqs, int vocab) {
   if (vocab > kRowBlocks * kBlockVals) return false;
-  return seqs >= kCus * 3 / 4 || vocab <= 32 * kBlockVals;
+  return seqs >= kCus * 3 / 4 || vocab <= 64 * kBlockVals;
 }
 
 template <typename T>
-hipError_t launch_verify(const VerifyArgs& a, BlockSum* ws, hipStream_t s) {
+hipError_t launch_verify(const VerifyArgs& a, double* ws, hipStream_t s) {
   const int blocks = (a.vocab + kBlockVals - 1) / kBlockVals;
   if (verify_by_rows(a.seqs, a.vocab)) {
     if (a.vocab < vec16<T>::kN)
@@ -596,7 +661,7 @@ hipError_t launch_verify(const VerifyArgs& a, BlockSum* ws, hipStream_t s) {
   }
   const int gx = std::max(1, std::min((blocks + 3) / 4, (8 * kCus + a.seqs - 1) / a.seqs));
   verify_sums_kernel<T><<<dim3(gx, a.seqs), 256, 0, s>>>(a, ws);
-  verify_pick_kernel<T><<<a.seqs, 64, 0, s>>>(a, ws);
+  verify_pick_kernel<T><<<a.seqs, 256, 0, s>>>(a, ws);
   return hipGetLastError();
 }
 
@@ -627,13 +692,13 @@ hipError_t token_probs(DType in_dt, const void* logits, int64_t ld_in, int rows,
 
 size_t verify_bytes(int seqs, int vocab) {
   if (verify_by_rows(seqs, vocab)) return 0;
-  return (size_t)seqs * ((vocab + kBlockVals - 1) / kBlockVals) * sizeof(BlockSum);
+  return (size_t)seqs * ((vocab + kBlockVals - 1) / kBlockVals) * sizeof(double);
 }
 
 hipError_t verify_drafts(DType dt, const VerifyArgs& a, void* ws, hipStream_t s) {
   if (a.seqs == 0) return hipSuccess;
-  if (dt == DT_F32) return launch_verify<float>(a, (BlockSum*)ws, s);
-  return launch_verify<bf16_t>(a, (BlockSum*)ws, s);
+  if (dt == DT_F32) return launch_verify<float>(a, (double*)ws, s);
+  return launch_verify<bf16_t>(a, (double*)ws, s);
 }
 
 }  // namespace stage_k

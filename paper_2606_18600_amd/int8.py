@@ -37,17 +37,18 @@ def unsupported(msg: str) -> S.StageError:
 
 def on_gpu(*tensors: Optional[torch.Tensor]) -> torch.device:
     """The GPU that all the tensors (None aside) are on."""
-    device = None
+    first, index = None, -1
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
-            raise invalid(f"a tensor is on {t.device}, not on a GPU")
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise invalid(f"tensors on {device} and {t.device}")
-    return device
+        i = t.get_device()
+        if i != index or i < 0:
+            if not t.is_cuda:
+                raise invalid(f"a tensor is on {t.device}, not on a GPU")
+            if first is not None:
+                raise invalid(f"tensors on {first.device} and {t.device}")
+            first, index = t, i
+    return first.device
 
 
 def is_current(device: torch.device) -> bool:

@@ -66,12 +66,6 @@ def token_probs(logits: torch.Tensor, temperature: Optional[torch.Tensor] = None
     return result
 
 
-def _array(t: torch.Tensor, n: int, dtype: torch.dtype, what: str) -> torch.Tensor:
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
-        raise invalid(f"{what} must be {dtype} [{n}], not {t.dtype} {tuple(t.shape)}")
-    return t.contiguous()
-
-
 def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor],
                   drafts: torch.Tensor, starts: torch.Tensor, max_drafts: int,
                   accept_u: torch.Tensor, sample_u: torch.Tensor
@@ -102,10 +96,14 @@ def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor
         raise invalid(f"draft_probs must be {target_probs.dtype} [{n}, {vocab}]")
     p = rows_of(target_probs, "target_probs")
     q = None if draft_probs is None else rows_of(draft_probs, "draft_probs")
-    drafts = _array(drafts, n, torch.int32, "drafts")
-    starts = _array(starts, seqs + 1, torch.int32, "starts")
-    accept_u = _array(accept_u, n, torch.float32, "accept_u")
-    sample_u = _array(sample_u, seqs, torch.float32, "sample_u")
+    i32, f32 = torch.int32, torch.float32
+    if drafts.dtype != i32 or starts.dtype != i32 or accept_u.dtype != f32 or \
+            sample_u.dtype != f32:
+        raise invalid("verify_drafts: drafts and starts must be int32, random numbers float32")
+    if accept_u.shape != (n,) or sample_u.shape != (seqs,):
+        raise invalid(f"verify_drafts: accept_u must be [{n}], sample_u [{seqs}]")
+    drafts, starts = drafts.contiguous(), starts.contiguous()
+    accept_u, sample_u = accept_u.contiguous(), sample_u.contiguous()
     if max_drafts < 0:
         raise invalid(f"max_drafts {max_drafts}")
     n_accepted = torch.empty(seqs, dtype=torch.int32, device=device)
