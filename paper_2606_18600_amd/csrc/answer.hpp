@@ -51,7 +51,8 @@ enum QuantKernel {
   QUANT_TILE_16X16,
   QUANT_TILE_8X8,
   QUANT_TILE_4X8,
-  QUANT_TILE_4X4
+  QUANT_TILE_4X4,
+  QUANT_TILE_4X4_K2  // two parts of k in a block: ranges of a multiple of 4 k tiles
 };
 constexpr int kStreamStrips = 4;   // row strips of 16 that the stream kernel takes
 constexpr int kSkinnyStrips = 12;  // ... and the skinny kernel

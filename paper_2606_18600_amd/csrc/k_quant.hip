@@ -594,7 +594,8 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(const int* __restrict
 // into a ring of R slots, R - 1 stages ahead. A wave multiplies in halves of its
 // columns; while it does, half of the next stage's rows and the other half's (the
 // next stage's) columns come out of LDS, six fragments a half on 8 x 4 strips, so
-// that LDS is read evenly. One barrier a stage publishes the copies of stage kt +
+// that LDS is read evenly. KG = 2: two such groups of waves on a half of the k range
+// each, for tiles too few to give a CU two blocks. One barrier a stage publishes the copies of stage kt +
 // 1 and frees the slot of stage kt - 1.
 //
 // Bound: power. 2048 x 57344 x 8192 takes 735 us (2.62 Pop/s; a library int8
@@ -602,15 +603,18 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(const int* __restrict
 // the time; with operands of zeros, hence little switching, 587 us. Measured
 // against it: 4 x 2 waves 750 us, reads in bursts 741, v_mfma_i32_32x32x32_i8 894,
 // four waves of 128 x 128 827, a ring of 5 759.
-template <int BM, int BN, int WM, int WN, int R, typename OutT>
-__global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
+template <int BM, int BN, int WM, int WN, int R, int KG, typename OutT>
+__global__ __launch_bounds__(KG * WM * WN * 64, 2) void quant_tiled_kernel(
     const char* __restrict__ A, const float* __restrict__ sa, const char* __restrict__ B,
     const float* __restrict__ sb, int M, int N, int KT, int kt_len, OutT* __restrict__ out,
     int64_t ldo) {
   constexpr int NW = WM * WN, FR = BM + BN, PW = FR / NW, TM = BM / WM, TN = BN / WN, TH = TN / 2;
   static_assert(FR % NW == 0 && BM % WM == 0 && BN % WN == 0 && TN % 2 == 0, "tile split");
-  __shared__ u32x4_t lds[R][FR * 64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  static_assert(KG <= 2, "two parts of k at most");
+  __shared__ u32x4_t ring[KG][R][FR * 64];
+  const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = all / NW, wave = all % NW;
+  u32x4_t (&lds)[R][FR * 64] = ring[kg];
   const int wm = wave / WN, wn = wave % WN;
   // Blocks go round-robin to the 8 XCDs, each with an L2 of its own: give an XCD
   // whole columns of tiles, so that a weight strip is fetched into one L2.
@@ -630,7 +634,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
   }
   const int ms = (M + 15) / 16, ns = (N + 15) / 16;
   const int m0 = mb * BM, n0 = nb * BN;
-  const int k0 = blockIdx.z * kt_len, kts = min(kt_len, KT - k0);  // this block's k tiles (even)
+  // this part's k tiles: an even number, the same for the parts of a block
+  const int kts = min(kt_len, KT - (int)blockIdx.z * kt_len) / KG;
+  const int k0 = blockIdx.z * kt_len + kg * kts;
   // fragment f of a stage: strip m0 + f of A, then strip n0 + f - BM of B (strips
   // past the end repeat the last one; nothing of theirs is stored)
   const char* src[PW];
@@ -702,6 +708,25 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void quant_tiled_kernel(
   }
   // copies past the end still write this block's LDS: they land before it ends
   __builtin_amdgcn_s_waitcnt(vmcnt_at_most(0));
+
+  if constexpr (KG > 1) {  // part 1 hands its sums to part 0
+    static_assert(TM * TN * NW <= R * FR, "the ring holds a part's sums");
+    __syncthreads();
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          ring[0][0][((wave * TM + i) * TN + j) * 64 + lane] = __builtin_bit_cast(u32x4_t, acc[i][j]);
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[i][j] += __builtin_bit_cast(i32x4_t, ring[0][0][((wave * TM + i) * TN + j) * 64 + lane]);
+  }
 
   // The products are transposed (weights as the first operand): lane l holds row
   // l % 16 and columns 4 (l / 16) .. + 3 of a tile, which it stores together.
@@ -793,11 +818,11 @@ void launch_skinny(const Product& p, OutT* out, int64_t ldo) {
           p.a, p.sa, p.b, p.sb, p.M, p.N, p.KT, p.plan.kt_len, out, ldo);
 }
 
-template <int BM, int BN, int WM, int WN, int R, typename OutT>
+template <int BM, int BN, int WM, int WN, int R, int KG, typename OutT>
 void launch_tiled(const Product& p, OutT* out, int64_t ldo) {
   const int strips = (p.N + 15) / 16, tiles = (p.M + 15) / 16;
-  quant_tiled_kernel<BM, BN, WM, WN, R, OutT>
-      <<<dim3((tiles + BM - 1) / BM, (strips + BN - 1) / BN, p.plan.ranges), WM * WN * 64, 0,
+  quant_tiled_kernel<BM, BN, WM, WN, R, KG, OutT>
+      <<<dim3((tiles + BM - 1) / BM, (strips + BN - 1) / BN, p.plan.ranges), KG * WM * WN * 64, 0,
          p.s>>>(p.a, p.sa, p.b, p.sb, p.M, p.N, p.KT, p.plan.kt_len, out, ldo);
 }
 
@@ -823,10 +848,11 @@ void launch_ranges(const Product& p, OutT* out, int64_t ldo) {
     case QUANT_SKINNY_4X2: launch_skinny_rows<4, 2>(p, out, ldo); break;
     case QUANT_SKINNY_4X4: launch_skinny_rows<4, 4>(p, out, ldo); break;
     case QUANT_SKINNY_4X8: launch_skinny_rows<4, 8>(p, out, ldo); break;
-    case QUANT_TILE_16X16: launch_tiled<16, 16, 2, 4, 4>(p, out, ldo); break;
-    case QUANT_TILE_8X8: launch_tiled<8, 8, 2, 2, 5>(p, out, ldo); break;
-    case QUANT_TILE_4X8: launch_tiled<4, 8, 2, 2, 6>(p, out, ldo); break;
-    default: launch_tiled<4, 4, 2, 2, 8>(p, out, ldo);
+    case QUANT_TILE_16X16: launch_tiled<16, 16, 2, 4, 4, 1>(p, out, ldo); break;
+    case QUANT_TILE_8X8: launch_tiled<8, 8, 2, 2, 5, 1>(p, out, ldo); break;
+    case QUANT_TILE_4X8: launch_tiled<4, 8, 2, 2, 6, 1>(p, out, ldo); break;
+    case QUANT_TILE_4X4: launch_tiled<4, 4, 2, 2, 8, 1>(p, out, ldo); break;
+    default: launch_tiled<4, 4, 2, 2, 8, 2>(p, out, ldo);
   }
 }
 

@@ -17,6 +17,7 @@
 //   skinny, 4 x 4       64 x 57344 x 8192      76.8 (skinny 4 x 2: 86.8)
 //   skinny, 4 x 8       64 x 128256 x 8192    158.3 (skinny 4 x 4: 184.9)
 //   tiles, 4 x 4        613 x 1277 x 2503       8.8 (tiles of 4 x 8: 11.6)
+//   ... two parts of k  256 x 4096 x 4096       9.3 (tiles of 4 x 4: 11.1)
 //   tiles, 4 x 8        150 x 10240 x 5120     20.4 (skinny 2 x 2: 24.4)
 //   tiles, 8 x 8        2048 x 2048 x 2048     12.6 (tiles of 4 x 8: 14.2)
 //   tiles, 16 x 16      2048 x 57344 x 8192     735 (tiles of 8 x 8: 958)
@@ -123,6 +124,11 @@ QuantPlan quant_plan(int M, int N, int K, size_t room, bool unquantised) {
       double us = full * (len * (t.two > 0 ? two : one) + t.ends);
       if (rest) us += len * (rest > kCus ? two : one) + t.ends;
       offer(t.kind, len, std::max(us, mb / 5.5));
+      // the smallest tile with two parts of k a block, one block on a CU
+      if (t.kind == QUANT_TILE_4X4 && len % 4 == 0 && KT % 4 == 0)
+        offer(QUANT_TILE_4X4_K2, len,
+              std::max(up(blocks, kCus) * (len / 2 * (weights > 4e7 ? 0.29 : 0.15) + 0.8),
+                       mb / 5.5));
     }
   return best;
 }
