@@ -124,11 +124,10 @@ QuantPlan quant_plan(int M, int N, int K, size_t room, bool unquantised) {
       double us = full * (len * (t.two > 0 ? two : one) + t.ends);
       if (rest) us += len * (rest > kCus ? two : one) + t.ends;
       offer(t.kind, len, std::max(us, mb / 5.5));
-      // the smallest tile with two parts of k a block, one block on a CU
-      if (t.kind == QUANT_TILE_4X4 && len % 4 == 0 && KT % 4 == 0)
+      // the smallest tile with two parts of k a block, where every block has a CU
+      if (t.kind == QUANT_TILE_4X4 && len % 4 == 0 && KT % 4 == 0 && blocks <= kCus)
         offer(QUANT_TILE_4X4_K2, len,
-              std::max(up(blocks, kCus) * (len / 2 * (weights > 4e7 ? 0.29 : 0.15) + 0.8),
-                       mb / 5.5));
+              std::max(len / 2 * (weights > 4e7 ? 0.29 : 0.15) + 0.8, mb / 5.5));
     }
   return best;
 }
