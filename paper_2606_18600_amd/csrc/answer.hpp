@@ -49,6 +49,7 @@ enum QuantKernel {
   QUANT_SKINNY_4X4,
   QUANT_SKINNY_4X8,
   QUANT_TILE_16X16,
+  QUANT_TILE_12X8,
   QUANT_TILE_8X8,
   QUANT_TILE_4X8,
   QUANT_TILE_4X4,

@@ -849,6 +849,7 @@ void launch_ranges(const Product& p, OutT* out, int64_t ldo) {
     case QUANT_SKINNY_4X4: launch_skinny_rows<4, 4>(p, out, ldo); break;
     case QUANT_SKINNY_4X8: launch_skinny_rows<4, 8>(p, out, ldo); break;
     case QUANT_TILE_16X16: launch_tiled<16, 16, 2, 4, 4, 1>(p, out, ldo); break;
+    case QUANT_TILE_12X8: launch_tiled<12, 8, 2, 2, 4, 1>(p, out, ldo); break;
     case QUANT_TILE_8X8: launch_tiled<8, 8, 2, 2, 5, 1>(p, out, ldo); break;
     case QUANT_TILE_4X8: launch_tiled<4, 8, 2, 2, 6, 1>(p, out, ldo); break;
     case QUANT_TILE_4X4: launch_tiled<4, 4, 2, 2, 8, 1>(p, out, ldo); break;

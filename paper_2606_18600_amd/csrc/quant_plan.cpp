@@ -20,6 +20,7 @@
 //   ... two parts of k  256 x 4096 x 4096       9.3 (tiles of 4 x 4: 11.1)
 //   tiles, 4 x 8        150 x 10240 x 5120     20.4 (skinny 2 x 2: 24.4)
 //   tiles, 8 x 8        2048 x 2048 x 2048     12.6 (tiles of 4 x 8: 14.2)
+//   tiles, 12 x 8       2204 x 2560 x 5120     32.4 (tiles of 8 x 8: 40.5)
 //   tiles, 16 x 16      2048 x 57344 x 8192     735 (tiles of 8 x 8: 958)
 #include <algorithm>
 
@@ -39,6 +40,7 @@ struct Tile {
   double one, two, ends;
 };
 constexpr Tile kTiles[] = {{QUANT_TILE_16X16, 16, 16, 4, 0.75, 0.0, 0.0},
+                           {QUANT_TILE_12X8, 12, 8, 4, 0.31, 0.66, 1.0},
                            {QUANT_TILE_8X8, 8, 8, 5, 0.22, 0.51, 1.1},
                            {QUANT_TILE_4X8, 4, 8, 6, 0.137, 0.36, 0.9},
                            {QUANT_TILE_4X4, 4, 4, 8, 0.087, 0.22, 0.8}};

@@ -95,7 +95,8 @@ def test_linear_wide_and_deep(m):
     (33, 57339, 2000), (64, 10239, 5120), (64, 128251, 1000), (70, 128251, 250), (100, 57339, 2000),
     (125, 128251, 900), (128, 10239, 5120), (128, 8191, 8192), (130, 57339, 2000),
     (150, 28670, 4096), (165, 57339, 515), (190, 128251, 700), (40, 5121, 20000),
-    (10, 12930, 9000), (1100, 40961, 200), (2050, 8200, 300), (2100, 20001, 160)])
+    (10, 12930, 9000), (1100, 40961, 200), (2050, 8200, 300), (2100, 20001, 160),
+    (2200, 2555, 300), (300, 8191, 8192)])
 def test_linear_many_columns(m, n, k):
     """Sizes that keep most of the chip at work, one or more for each kernel; all rows,
     a sample of columns with the first and the last."""
