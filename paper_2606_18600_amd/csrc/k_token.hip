@@ -1,6 +1,7 @@
 // From logits to tokens: probabilities at a temperature, and the verification
 // of drafted tokens against them.
 #include <algorithm>
+#include <type_traits>
 
 #include "answer.hpp"
 #include "common.hpp"
@@ -103,8 +104,8 @@ __device__ __forceinline__ void store_vec(T* row, int k, int at, int n, const fl
 // probabilities
 // ---------------------------------------------------------------------------
 // p = exp((x - max) / T) / sum, statistics in fp32. A row of up to kRowVals values
-// stays in the registers of one block. A longer one is cut into pieces of kPiece
-// values, a block each: one pass for the pieces' maxima, sums and first places of
+// stays in the registers of one block, and of many rows in fp32 one of up to
+// kBigVals. Others are cut into pieces of kPiece values, a block each: one pass for the pieces' maxima, sums and first places of
 // the maximum, a second that joins a row's pieces (in their order) and writes.
 // Masked logits (-inf) get 0, a row of nothing else zeros throughout.
 //
@@ -114,6 +115,7 @@ __device__ __forceinline__ void store_vec(T* row, int k, int at, int n, const fl
 constexpr int kThreadVals = 32;
 constexpr int kPiece = 256 * kThreadVals;
 constexpr int kRowVals = 1024 * kThreadVals;
+constexpr int kBigVals = 1024 * 128;
 constexpr float kMinT = 0x1p-100f, kMaxT = 0x1p100f;  // (x - max) / T stays ordered
 
 struct Piece {
@@ -157,6 +159,26 @@ __device__ __forceinline__ int place(int begin, int n, int j) {
   return vec_at<V, kShort>(begin + (j * THREADS + threadIdx.x) * V, n);
 }
 
+// The statistics of a block's NW waves, joined; every thread gets them.
+template <int NW>
+__device__ __forceinline__ void join_waves(float& m, float& s, int& at, float c) {
+  __shared__ float sm[NW], ss[NW];
+  __shared__ int sat[NW];
+  if ((threadIdx.x & 63) == 0) {
+    const int w = threadIdx.x >> 6;
+    sm[w] = m, ss[w] = s, sat[w] = at;
+  }
+  __syncthreads();
+  const int w = threadIdx.x % NW;
+  m = sm[w], s = ss[w], at = sat[w];
+#pragma unroll
+  for (int o = 1; o < NW; o <<= 1) {
+    const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
+    const int at2 = __shfl_xor(at, o, 64);
+    join(m, s, at, m2, s2, at2, c);
+  }
+}
+
 // The values' maximum, the sum of exp((v - max) / T) and, on a greedy row, the first
 // place of the maximum; every thread gets them.
 template <int NV, int V, int THREADS, bool kShort>
@@ -188,21 +210,7 @@ __device__ __forceinline__ void piece_stats(const float (&v)[NV][V], int begin, 
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) at = min(at, __shfl_xor(at, o, 64));
   }
-  __shared__ float sm[NW], ss[NW];
-  __shared__ int sat[NW];
-  if ((threadIdx.x & 63) == 0) {
-    const int w = threadIdx.x >> 6;
-    sm[w] = m, ss[w] = s, sat[w] = at;
-  }
-  __syncthreads();
-  const int w = threadIdx.x % NW;
-  m = sm[w], s = ss[w], at = sat[w];
-#pragma unroll
-  for (int o = 1; o < NW; o <<= 1) {
-    const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
-    const int at2 = __shfl_xor(at, o, 64);
-    join(m, s, at, m2, s2, at2, c);
-  }
+  join_waves<NW>(m, s, at, c);
 }
 
 // The values' probabilities, given their row's statistics. On a greedy row s is NaN
@@ -278,6 +286,112 @@ __global__ __launch_bounds__(256) void probs_write_kernel(const T* logits, int64
   store_probs<NV, V, 256, false>(v, begin, vocab, slope, m, s, at, probs + (int64_t)row * ld_out);
 }
 
+// Rows of up to kBigVals fp32 values by one block of 1024 threads: NREG vectors of
+// 16 bytes a thread in registers, NLDS in LDS. Against two passes over pieces it
+// reads a row once, at a CU's pace: 32 rows of 128256 take 21.9 us (12.5), 128 28.6
+// (33.5), 256 50.6 (63.8; 5.2 TB/s), 300 70.3 (73.4), 700 140 (185); 128 and 256 of
+// 64000 15.1 (16.7) and 25.0 (31.7). (bf16 rows gain nothing: 320 of them to fp32 87
+// against 71.)
+template <typename OutT, int NREG, int NLDS>
+__global__ __launch_bounds__(1024) void probs_big_kernel(const float* logits, int64_t ld,
+                                                         int vocab,
+                                                         const float* __restrict__ temperature,
+                                                         OutT* probs, int64_t ld_out) {
+  typedef float T;
+  constexpr int V = vec16<T>::kN;
+  __shared__ vec16<T> kept[NLDS > 0 ? NLDS * 1024 : 1];
+  const int row = blockIdx.x;
+  const T* x = logits + (int64_t)row * ld;
+  const float slope = row_slope(temperature, row);
+  const float c = slope > 0.f ? slope : 1.44269504088896341f;
+  // The empty asm statements below make the compiler compute places and values again
+  // in every pass over the row: kept from pass to pass they would spill.
+  int tid = threadIdx.x;
+  auto start = [&](int j) { return (j * 1024 + tid) * V; };
+  auto read = [&](int j) {
+    vec16<T> v;
+    read_vec<false>(x, start(j), vocab, v);
+    return v;
+  };
+  auto trim = [&](int j, vec16<T>& v) {  // as trim_vec
+    const int k = start(j);
+    if (k + V <= vocab) return;
+    const int at = vec_at<V, false>(k, vocab);
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (at + e < k) v.set(e, -INFINITY);
+  };
+  vec16<T> v[NREG];
+  if constexpr (NLDS > 0) {
+    vec16<T> t[NLDS];
+#pragma unroll
+    for (int j = 0; j < NLDS; ++j) t[j] = read(NREG + j);
+#pragma unroll
+    for (int j = 0; j < NLDS; ++j) {
+      trim(NREG + j, t[j]);
+      kept[j * 1024 + tid] = t[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NREG; ++j) v[j] = read(j);
+#pragma unroll
+  for (int j = 0; j < NREG; ++j) trim(j, v[j]);
+  float m = -INFINITY, s = 0.f;
+  auto each = [&](auto f) {
+    asm volatile("" : "+v"(tid));
+#pragma unroll
+    for (int j = 0; j < NREG; ++j) {
+      asm volatile("" : "+v"(v[j].w));
+      f(j, v[j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int j = 0; j < NLDS; ++j) {
+      f(NREG + j, kept[j * 1024 + tid]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  each([&](int, const vec16<T>& w) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) m = fmaxf(m, w.get(e));
+  });
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  {
+    const float base = m == -INFINITY ? 0.f : m;
+    each([&](int, const vec16<T>& w) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) s += __builtin_amdgcn_exp2f((w.get(e) - base) * c);
+    });
+  }
+  s = wave_sum(s);
+  int best = INT32_MAX;
+  if (slope == 0.f) {
+    each([&](int j, const vec16<T>& w) {
+      const int at = vec_at<V, false>(start(j), vocab);
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (w.get(e) == m) best = min(best, at + e);
+    });
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) best = min(best, __shfl_xor(best, o, 64));
+  }
+  join_waves<16>(m, s, best, c);
+  const float base = m == -INFINITY ? 0.f : m;
+  const float inv = s == 0.f ? 0.f : 1.0f / s;
+  OutT* p = probs + (int64_t)row * ld_out;
+  each([&](int j, const vec16<T>& w) {
+    const int k = start(j), at = vec_at<V, false>(k, vocab);
+    float o[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      o[e] = slope > 0.f ? __builtin_amdgcn_exp2f((w.get(e) - base) * slope) * inv
+             : s > 0.f   ? (at + e == best ? 1.f : 0.f)
+                         : s;
+    store_vec<V>(p, k, at, vocab, o);
+  });
+}
+
 template <typename T, typename OutT>
 hipError_t launch_probs(const T* x, int64_t ld, int rows, int vocab, const float* t, OutT* out,
                         int64_t ld_out, Piece* ws, hipStream_t s) {
@@ -292,6 +406,17 @@ hipError_t launch_probs(const T* x, int64_t ld, int rows, int vocab, const float
   if (vocab <= kRowVals) {
     probs_row_kernel<T, OutT, 1024, false><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
     return hipGetLastError();
+  }
+  if constexpr (std::is_same<T, float>::value) {
+    if (vocab <= kBigVals && rows >= kCus / 2) {
+      if (vocab <= 1024 * 4 * 16)
+        probs_big_kernel<OutT, 16, 0><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
+      else if (vocab <= 1024 * 4 * 24)
+        probs_big_kernel<OutT, 23, 1><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
+      else
+        probs_big_kernel<OutT, 23, 9><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
+      return hipGetLastError();
+    }
   }
   const int pieces = (vocab + kPiece - 1) / kPiece;
   for (int r = 0; r < rows; r += 65535) {  // the grid's limit

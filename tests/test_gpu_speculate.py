@@ -64,7 +64,9 @@ def _logits(seed, rows, vocab, dtype="f32", scale=4.0):
 @pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (2, 7), (5, 63), (1, 1000), (7, 1024),
                                         (2, 4097), (33, 8191), (4, 8192), (3, 8193), (2, 32003),
                                         (300, 515), (1, 65537), (2, 128256), (270, 16400),
-                                        (260, 50001), (1, 300001)])
+                                        (260, 50001), (1, 300001), (128, 32769), (130, 65535),
+                                        (129, 65537), (140, 98304), (128, 98305), (131, 131072),
+                                        (128, 131073)])
 @pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"),
                                        ("bf16", "bf16")])
 def test_token_probs(rows, vocab, dtype, out):
@@ -103,6 +105,29 @@ def test_masks_infinities_and_greedy_ties(vocab, dtype):
     greedy = speculate.token_probs(x, t * 0)
     assert greedy[9, 5] == 1 and greedy[10, 0] == 1 and greedy[11, vocab - 2] == 1
     assert (greedy[1] == 0).all() and greedy.nansum(1)[[0, 2, 3, 4, 5, 6]].eq(1).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(128, 50003), (150, 128256)])
+def test_masks_in_many_long_rows(rows, vocab):
+    """The same where one block holds a row."""
+    x = _logits(vocab, rows, vocab)
+    low = torch.finfo(torch.float32).min
+    x[0, ::2], x[1, :], x[2, :], x[3, :] = -INF, -INF, -INF, low
+    x[2, vocab - 1] = low
+    x[5, : vocab // 2], x[6, 17:] = -INF, -INF
+    x[7, vocab // 3], x[8, vocab - 1] = float("nan"), INF
+    x[9, 5], x[9, vocab - 1], x[9, vocab // 2] = 90.0, 90.0, 90.0
+    x[10, :] = 0.0
+    x[11, vocab - 2:] = 60.0
+    t = torch.full((rows,), 0.8, device="cuda")
+    for temperature in (None, t, t * 0):
+        _probs_close(speculate.token_probs(x, temperature), x, temperature, "f32")
+    wide = torch.full((rows, vocab + 7), -3.0, device="cuda")
+    wide[:, 3:3 + vocab] = x
+    y = speculate.token_probs(x, t)
+    z = speculate.token_probs(wide[:, 3:3 + vocab], t, out=wide[:, 3:3 + vocab])
+    assert torch.equal(y.nan_to_num(2.0), z.nan_to_num(2.0))
+    assert (wide[:, :3] == -3).all() and (wide[:, 3 + vocab:] == -3).all()
 
 
 @pytest.mark.parametrize("vocab", [300, 8195, 40000])
