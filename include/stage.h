@@ -296,12 +296,14 @@ stage_status stage_pack_lm_head(const stage_model_config* cfg, int32_t vocab, co
  *    product NaN, and no other.
  *  - Sums are exact (int32; k <= 131072, else STAGE_ERR_UNSUPPORTED); then
  *    out = sum * (scale_a * scale_b) in float32, rounded once to out_dtype.
- *  - Any rows, k and n from 1 on (rows or n 0: nothing is done); row strides
+ *  - Any k from 1 and rows and n up to 2^21 (0: nothing is done); row strides
  *    (ld, in elements, >= the row's length) and addresses as the types allow.
  *    Output and inputs must not overlap.
- *  - These calls, and those of the next section, need no stage: they run on the
- *    current device, whose memory their pointers name and whose stream `stream`
- *    is. They keep nothing between calls and may be captured into a graph. */
+ *  - These calls (stage_lm_head_quant aside), and those of the next section,
+ *    need no stage: they run on the current device, whose memory their pointers
+ *    name and whose stream `stream` is. They keep nothing between calls, may run
+ *    on several streams at once (each with scratch of its own) and may be captured
+ *    into a graph. */
 
 /* Bytes of a quantised [rows, k] matrix; 0 if the size is not supported. */
 size_t stage_quant_bytes(int32_t rows, int32_t k);
@@ -334,8 +336,7 @@ stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, in
 
 /* stage_lm_head with W_lm as a quantised [vocab, hidden] matrix: the normed
  * rows are quantised from float32 (they are not rounded to the mode dtype
- * first). Any vocab >= 1; everything else as for stage_lm_head, the pointers
- * hidden and final_norm 16-byte aligned. */
+ * first). Any vocab from 1 to 2^21; everything else as for stage_lm_head. */
 stage_status stage_lm_head_quant(stage_t* st, const void* final_norm, const void* w_lm,
                                  int32_t vocab, const void* hidden, int32_t hidden_rows,
                                  const int32_t* rows, int32_t n_rows, float* logits,

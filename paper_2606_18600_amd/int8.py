@@ -12,7 +12,8 @@ matrices::
 A quantised weight [vocab, hidden] also serves as the LM head's
 (``harness.DeviceStage.lm_head``). Everything runs on torch's current stream of
 the tensors' device; outputs and scratch come from torch's allocator, so calls
-may be captured into a graph.
+may be captured into a graph. There is no backward pass: results carry no
+gradient.
 """
 
 from __future__ import annotations

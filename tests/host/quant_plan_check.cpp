@@ -1,0 +1,73 @@
+// Checks the plans of 8-bit products (csrc/quant_plan.cpp) over many sizes (test
+// code only). Exit status 0 and a last line "plans passed" on success.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+
+#include "../../paper_2606_18600_amd/csrc/answer.hpp"
+
+using namespace stage_k;
+
+namespace {
+
+void check(bool ok, const char* what, int M, int N, int K, const QuantPlan& p) {
+  if (ok) return;
+  std::printf("%s: %d x %d x %d: kernel %d, %d ranges of %d\n", what, M, N, K, (int)p.kernel,
+              p.ranges, p.kt_len);
+  std::exit(1);
+}
+
+long up(long a, long b) { return (a + b - 1) / b; }
+
+void check_plan(int M, int N, int K, size_t room, bool rows) {
+  const QuantPlan p = quant_plan(M, N, K, room, rows);
+  const long KT = (long)quant_kp(K) / 64, strips = up(N, 16), tiles = up(M, 16);
+  check(p.ranges >= 1 && p.kt_len >= 1, "empty plan", M, N, K, p);
+  check((long)p.kt_len * p.ranges >= KT && (long)p.kt_len * (p.ranges - 1) < KT, "ranges", M, N, K,
+        p);
+  check(quant_plane_bytes(p, M, N) <= room, "room", M, N, K, p);
+  check(!p.fused || (rows && M <= kFusedRows && p.kernel <= QUANT_STREAM_3), "fused", M, N, K, p);
+  check(p.fused || p.kernel != QUANT_STREAM_2, "two strips", M, N, K, p);
+  int bn = 1, kp = 2;
+  switch (p.kernel) {
+    case QUANT_STREAM_1:
+    case QUANT_STREAM_2:
+    case QUANT_STREAM_3:
+      check(p.ranges == 1 && tiles <= kStreamStrips, "stream", M, N, K, p);
+      break;
+    case QUANT_SKINNY_2X2:
+    case QUANT_SKINNY_4X2:
+    case QUANT_SKINNY_4X4:
+    case QUANT_SKINNY_4X8:
+      kp = p.kernel == QUANT_SKINNY_4X8 ? 1 : p.kernel == QUANT_SKINNY_4X4 ? 2 : 4;
+      check(tiles <= kSkinnyStrips && (p.kernel != QUANT_SKINNY_4X8 || tiles > 1), "skinny", M, N,
+            K, p);
+      check(p.ranges == 1 || p.kt_len % kp == 0, "skinny range", M, N, K, p);
+      break;
+    default:
+      kp = p.kernel == QUANT_TILE_4X4_K2 ? 4 : 2;
+      bn = p.kernel == QUANT_TILE_16X16 ? 16 : p.kernel == QUANT_TILE_4X4 || kp == 4 ? 4 : 8;
+      check(p.kt_len % kp == 0 && KT % kp == 0, "tile range", M, N, K, p);
+      check(up(strips, bn) <= 65535, "grid", M, N, K, p);
+  }
+}
+
+}  // namespace
+
+int main() {
+  std::mt19937 rng(7);
+  std::uniform_real_distribution<double> u(0.0, 1.0);
+  auto draw = [&](double lo, double hi) { return (int)(lo * std::pow(hi / lo, u(rng)) + 0.5); };
+  const int edge[] = {1, 2, 15, 16, 17, 63, 64, 65, 128, 192, 193, 256, 1 << 21};
+  for (int i = 0; i < 20000; ++i) {
+    int M = draw(1, 5000), N = draw(1, 300000), K = draw(1, 131072);
+    if (i % 5 == 0) M = edge[rng() % 13];
+    if (i % 7 == 0) N = edge[rng() % 13];
+    if (i % 11 == 0) K = edge[rng() % 12];
+    check_plan(M, N, K, i % 3 == 0 ? (size_t)draw(1, 1 << 28) : SIZE_MAX, i % 2 == 0);
+  }
+  std::printf("plans passed\n");
+}

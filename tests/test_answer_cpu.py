@@ -5,13 +5,16 @@ device, with the documented code and a message. Pointers are never read."""
 from __future__ import annotations
 
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
 
-from paper_2606_18600_amd import int8, speculate
+from paper_2606_18600_amd import build, int8, speculate
 from paper_2606_18600_amd import stage as S
-from tests.test_abi_cpu import _lib
+from tests.test_abi_cpu import ROOT, _lib
 
 A, B, C, D = 0x10000, 0x20000, 0x30000, 0x40000   # 16-byte aligned, never dereferenced
 INV, UNS, CAP = S.STAGE_ERR_INVALID_ARG, S.STAGE_ERR_UNSUPPORTED, S.STAGE_ERR_CAPACITY
@@ -30,7 +33,7 @@ def test_quant_bytes():
     assert S.stage_quant_bytes(17, 129) == 32 * 256 + 32 * 4
     assert S.stage_quant_bytes(128256, 8192) == 128256 * 8192 + 128256 * 4
     assert S.stage_quant_bytes(0, 64) == 0
-    for rows, k in ((-1, 64), (4, 0), (4, 131073), ((1 << 24) + 1, 64)):
+    for rows, k in ((-1, 64), (4, 0), (4, 131073), ((1 << 21) + 1, 64)):
         assert S.stage_quant_bytes(rows, k) == 0
 
 
@@ -116,7 +119,7 @@ def test_lm_head_quant_refuses():
     lib = _lib()
     _refused(lib.stage_lm_head_quant(None, A, B, 1000, C, 4, None, 4, D, None), INV)
     _refused(lib.stage_lm_head_quant(None, A, B + 4, 1000, C, 4, None, 4, D, None), INV)
-    _refused(lib.stage_lm_head_quant(None, A, B, 1 << 25, C, 4, None, 4, D, None), UNS)
+    _refused(lib.stage_lm_head_quant(None, A, B, (1 << 21) + 1, C, 4, None, 4, D, None), UNS)
 
 
 @pytest.mark.parametrize("args,code", [
@@ -202,3 +205,44 @@ def test_tensor_calls_refuse():
     assert _code(speculate.verify_drafts, *args) == INV    # on the CPU
     assert _code(speculate.verify_drafts, h, *args[1:]) == UNS
     assert _code(speculate.verify_drafts, *args[:2], i.view(3, 1), *args[3:]) == INV
+
+
+def test_product_plans(tmp_path):
+    """The rule that picks a product's kernel, over 20000 sizes (host code, built with
+    g++ against a stand-in of the HIP header): ranges cover k exactly and none is
+    empty, their lengths fit the kernel, grids and planes stay within their limits."""
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("g++ not available")
+    exe = str(tmp_path / "quant_plan_check")
+    r = subprocess.run([gxx, "-std=c++17", "-O1", "-fsanitize=address,undefined",
+                        "-fno-sanitize-recover=all", "-I",
+                        os.path.join(ROOT, "tests", "host", "include"),
+                        os.path.join(ROOT, "tests", "host", "quant_plan_check.cpp"),
+                        os.path.join(build.SRC, "quant_plan.cpp"), "-o", exe],
+                       capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "plans passed" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+def test_matrix_instructions_are_not_masked(tmp_path):
+    """A matrix instruction ignores the lane mask, so one inside a divergent branch runs
+    for the lanes that did not take it, unless the branch is skipped where no lane
+    takes it. The conditions around the products of csrc/k_quant.hip are scalar: in
+    the built code no instruction follows a mask without such a skip."""
+    out = str(tmp_path / "k_quant.s")
+    r = subprocess.run([build.hipcc(), *build.HIPCC_FLAGS, "-x", "hip", "--cuda-device-only", "-S",
+                        os.path.join(build.SRC, "k_quant.hip"), "-o", out],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    masked, products = False, 0
+    for line in open(out):
+        if "s_and_saveexec" in line:
+            masked = True
+        elif "s_cbranch_execz" in line or "s_or_b64 exec" in line or line.startswith(".LBB"):
+            masked = False
+        elif "v_mfma_i32" in line:
+            products += 1
+            assert not masked, line
+    assert products > 1000

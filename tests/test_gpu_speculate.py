@@ -302,6 +302,32 @@ def test_empty_and_strange_rows():
     _check(args, su=torch.full((12,), -1.0, device="cuda"))
 
 
+@pytest.mark.parametrize("seqs", [3, 200])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nothing_left_of_long_rows(seqs, dtype):
+    """Rows longer than one block sums at once, drawn by two launches or by whole rows:
+    target rows of zeros, below the draft's everywhere, with infinities, and with all
+    their weight in the last token."""
+    vocab = 70001
+    args = _drafts(43, [1] * seqs, vocab, dtype)
+    p, q, d = args["p"], args["q"], args["drafts"]
+    p[0:2] = 0
+    p[2], p[3] = q[1] / 4, 0
+    q[1] = 1.0
+    p[4:6, 60000], p[4:6, 3] = INF, float("nan")
+    d[2] = 60000
+    if seqs > 3:
+        p[6:8] = 0
+        p[6:8, vocab - 1] = 1e-30
+        d[3] = 0
+    for draft in (q, None):
+        for u in (0.0, 0.7, 1.0 - 2.0 ** -24):
+            _, tokens = _check(args, p=p, q=draft, drafts=d,
+                               au=torch.full((seqs,), 0.9999, device="cuda"),
+                               su=torch.full((seqs,), u, device="cuda"))
+            assert tokens[0].tolist() == [-1, -1]
+
+
 @pytest.mark.parametrize("starts", [[-5, 3, 2, 9, 400], [0, 0, 0, 0, 0], [9, 9, 9, 9, 9],
                                     [400, -400, 400, -400, 400], [3, 1, 8, 8, 2]])
 def test_offsets_out_of_range_are_clamped(starts):
