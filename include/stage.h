@@ -294,8 +294,10 @@ stage_status stage_pack_lm_head(const stage_model_config* cfg, int32_t vocab, co
  *    rint(x * (1 / s)), each step rounded to nearest in float32. A row that
  *    holds a NaN or an infinity makes its row (for weights: column) of every
  *    product NaN, and no other.
- *  - Sums are exact (int32; k <= 131072, else STAGE_ERR_UNSUPPORTED); then
- *    out = sum * (scale_a * scale_b) in float32, rounded once to out_dtype.
+ *  - Sums are exact (int32; k <= 131072, else STAGE_ERR_UNSUPPORTED; at that k,
+ *    rows of -128 throughout, which only quant_pack can bring, times each other
+ *    would be one too large); then out = sum * (scale_a * scale_b) in float32,
+ *    rounded once to out_dtype.
  *  - Any k from 1 and rows and n up to 2^21 (0: nothing is done); row strides
  *    (ld, in elements, >= the row's length) and addresses as the types allow.
  *    Output and inputs must not overlap.
@@ -373,7 +375,7 @@ typedef struct {
   int32_t vocab;
   int32_t num_seqs;          /* at most 65535 */
   int32_t num_drafts;        /* of all sequences: starts[num_seqs] */
-  int32_t max_drafts;        /* of one sequence */
+  int32_t max_drafts;        /* of one sequence; at most 2^24 */
   const void* target_probs;  /* [num_drafts + num_seqs, vocab], row stride ld_target */
   int64_t ld_target;
   const void* draft_probs;   /* [num_drafts, vocab], row stride ld_draft: what each

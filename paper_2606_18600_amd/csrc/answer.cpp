@@ -18,6 +18,7 @@ constexpr int64_t kMaxLd = (int64_t)1 << 40;  // row offsets stay far below 2^63
 constexpr int kMaxQuantRows = 1 << 21;  // strips of 16, four a block, in a grid dimension
 constexpr int kMaxSeqs = 65535;  // a grid dimension
 constexpr int kMaxVocab = 1 << 30;
+constexpr int kMaxDrafts = 1 << 24;  // of one sequence: places in a row of tokens stay int32
 
 stage_status op_fail(stage_status code, const char* fmt, ...) {
   char buf[512];
@@ -224,6 +225,8 @@ stage_status stage_verify_drafts(const stage_drafts* b, int32_t* n_accepted, int
     return op_fail(STAGE_ERR_UNSUPPORTED, "vocab %d > %d", b->vocab, kMaxVocab);
   if (b->num_seqs > kMaxSeqs)
     return op_fail(STAGE_ERR_CAPACITY, "%d sequences > %d", b->num_seqs, kMaxSeqs);
+  if (b->max_drafts > kMaxDrafts)
+    return op_fail(STAGE_ERR_CAPACITY, "%d drafts of a sequence > %d", b->max_drafts, kMaxDrafts);
   if (b->num_drafts > INT32_MAX - b->num_seqs)
     return op_fail(STAGE_ERR_CAPACITY, "%d drafts of %d sequences", b->num_drafts, b->num_seqs);
   if (b->num_seqs == 0) return STAGE_OK;

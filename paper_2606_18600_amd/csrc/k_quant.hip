@@ -29,12 +29,13 @@ __device__ __forceinline__ size_t chunk_offset(int row, int kc, int KT) {
 // s = max(max_k |x_k| / 127, 2^-120), q_k = rint(x_k * (1 / s)): division and
 // products rounded to nearest in fp32, so every implementation of the formula
 // gets the same integers. The floor keeps 1 / s finite for rows of zeros. The
-// maximum is taken over the values' bits, whose order puts NaN above infinity:
-// a row with either gets a scale that is not finite, hence outputs of NaN,
-// and no other row is touched.
+// maximum is taken over the values' bits, whose order puts infinity and then NaN
+// above every number: a row with either gets a scale of NaN, hence outputs of NaN
+// whatever its integers are, and no other row is touched.
 constexpr float kMinScale = 0x1p-120f;
 
 __device__ __forceinline__ float row_scale(uint32_t max_bits) {
+  if (max_bits >= 0x7f800000u) return __builtin_nanf("");
   const float s = __uint_as_float(max_bits) / 127.0f;
   return s < kMinScale ? kMinScale : s;
 }

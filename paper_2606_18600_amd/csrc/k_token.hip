@@ -105,8 +105,9 @@ __device__ __forceinline__ void store_vec(T* row, int k, int at, int n, const fl
 // ---------------------------------------------------------------------------
 // p = exp((x - max) / T) / sum, statistics in fp32. A row of up to kRowVals values
 // stays in the registers of one block, and of many rows in fp32 one of up to
-// kBigVals. Others are cut into pieces of kPiece values, a block each: one pass for the pieces' maxima, sums and first places of
-// the maximum, a second that joins a row's pieces (in their order) and writes.
+// kBigVals. Others are cut into pieces of kPiece values, a block each: one pass for
+// the pieces' maxima, sums and first places of the maximum, a second that joins a
+// row's pieces (in their order) and writes.
 // Masked logits (-inf) get 0, a row of nothing else zeros throughout.
 //
 // Bound: memory. The probabilities are stored past the caches: with plain stores
@@ -392,20 +393,21 @@ __global__ __launch_bounds__(1024) void probs_big_kernel(const float* logits, in
   });
 }
 
+// Up to kLaunchRows rows.
 template <typename T, typename OutT>
-hipError_t launch_probs(const T* x, int64_t ld, int rows, int vocab, const float* t, OutT* out,
-                        int64_t ld_out, Piece* ws, hipStream_t s) {
+void launch_probs_rows(const T* x, int64_t ld, int rows, int vocab, const float* t, OutT* out,
+                       int64_t ld_out, Piece* ws, hipStream_t s) {
   if (vocab < vec16<T>::kN) {
     probs_row_kernel<T, OutT, 256, true><<<rows, 256, 0, s>>>(x, ld, vocab, t, out, ld_out);
-    return hipGetLastError();
+    return;
   }
   if (vocab <= 256 * kThreadVals) {
     probs_row_kernel<T, OutT, 256, false><<<rows, 256, 0, s>>>(x, ld, vocab, t, out, ld_out);
-    return hipGetLastError();
+    return;
   }
   if (vocab <= kRowVals) {
     probs_row_kernel<T, OutT, 1024, false><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
-    return hipGetLastError();
+    return;
   }
   if constexpr (std::is_same<T, float>::value) {
     if (vocab <= kBigVals && rows >= kCus / 2) {
@@ -415,19 +417,23 @@ hipError_t launch_probs(const T* x, int64_t ld, int rows, int vocab, const float
         probs_big_kernel<OutT, 23, 1><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
       else
         probs_big_kernel<OutT, 23, 9><<<rows, 1024, 0, s>>>(x, ld, vocab, t, out, ld_out);
-      return hipGetLastError();
+      return;
     }
   }
-  const int pieces = (vocab + kPiece - 1) / kPiece;
-  for (int r = 0; r < rows; r += 65535) {  // the grid's limit
-    const dim3 grid(pieces, std::min(rows - r, 65535));
-    const T* xr = x + (int64_t)r * ld;
-    const float* tr = t ? t + r : nullptr;
-    Piece* wr = ws + (size_t)r * pieces;
-    probs_piece_kernel<T><<<grid, 256, 0, s>>>(xr, ld, vocab, tr, wr);
-    probs_write_kernel<T, OutT>
-        <<<grid, 256, 0, s>>>(xr, ld, vocab, tr, wr, out + (int64_t)r * ld_out, ld_out);
-  }
+  const dim3 grid((vocab + kPiece - 1) / kPiece, rows);
+  probs_piece_kernel<T><<<grid, 256, 0, s>>>(x, ld, vocab, t, ws);
+  probs_write_kernel<T, OutT><<<grid, 256, 0, s>>>(x, ld, vocab, t, ws, out, ld_out);
+}
+
+constexpr int kLaunchRows = 65535;  // a grid dimension
+
+template <typename T, typename OutT>
+hipError_t launch_probs(const T* x, int64_t ld, int rows, int vocab, const float* t, OutT* out,
+                        int64_t ld_out, Piece* ws, hipStream_t s) {
+  const size_t pieces = (vocab + kPiece - 1) / kPiece;
+  for (int64_t r = 0; r < rows; r += kLaunchRows)
+    launch_probs_rows(x + r * ld, ld, (int)std::min<int64_t>(rows - r, kLaunchRows), vocab,
+                      t ? t + r : nullptr, out + r * ld_out, ld_out, ws + (size_t)r * pieces, s);
   return hipGetLastError();
 }
 

@@ -71,9 +71,11 @@ def scratch(n: int, device: torch.device) -> torch.Tensor:
 def rows_of(x: torch.Tensor, what: str) -> torch.Tensor:
     """x as [rows, k] with adjacent values in a row."""
     if x.dim() != 2:
-        if x.dim() == 0:
-            raise invalid(f"{what} has no dimension")
+        if x.dim() == 0 or x.shape[-1] == 0:
+            raise invalid(f"{what} {tuple(x.shape)} has no row")
         x = x.reshape(-1, x.shape[-1])
+    if max(x.shape) >= 1 << 31:  # the library's sizes are 32 bits wide
+        raise unsupported(f"{what}: {x.shape[0]} rows of {x.shape[1]}")
     if not x.is_contiguous():
         rows, k = x.shape
         if (k > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < k):

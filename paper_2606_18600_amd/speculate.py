@@ -24,6 +24,8 @@ from . import stage as S
 from .int8 import (DTYPES, check_out, invalid, is_current, on_gpu, row_stride, rows_of, scratch,
                    stream_of, unsupported)
 
+MAX_DRAFTS = 1 << 24  # of one sequence
+
 _probs_bytes = lru_cache(4096)(S.stage_token_probs_bytes)
 _verify_bytes = lru_cache(4096)(S.stage_verify_bytes)
 
@@ -104,7 +106,7 @@ def verify_drafts(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor
         raise invalid(f"verify_drafts: accept_u must be [{n}], sample_u [{seqs}]")
     drafts, starts = drafts.contiguous(), starts.contiguous()
     accept_u, sample_u = accept_u.contiguous(), sample_u.contiguous()
-    if max_drafts < 0:
+    if not 0 <= max_drafts <= MAX_DRAFTS:
         raise invalid(f"max_drafts {max_drafts}")
     n_accepted = torch.empty(seqs, dtype=torch.int32, device=device)
     tokens = torch.empty((seqs, max_drafts + 1), dtype=torch.int32, device=device)

@@ -158,7 +158,8 @@ def test_workspaces_are_checked():
 @pytest.mark.parametrize("field,value,code", [
     ("dtype", 9, UNS), ("vocab", 0, INV), ("vocab", (1 << 30) + 1, UNS), ("num_seqs", -1, INV),
     ("num_seqs", 65536, CAP), ("num_drafts", -1, INV), ("num_drafts", (1 << 31) - 2, CAP),
-    ("max_drafts", -1, INV), ("target_probs", 0, INV), ("target_probs", A + 2, INV),
+    ("max_drafts", -1, INV), ("max_drafts", (1 << 24) + 1, CAP),
+    ("max_drafts", (1 << 31) - 1, CAP), ("target_probs", 0, INV), ("target_probs", A + 2, INV),
     ("ld_target", 63, INV), ("ld_draft", 63, INV), ("draft_probs", B + 1, INV), ("drafts", 0, INV),
     ("drafts", C + 2, INV), ("starts", 0, INV), ("accept_u", 0, INV), ("sample_u", 0, INV),
     ("sample_u", C + 1, INV),
@@ -205,6 +206,14 @@ def test_tensor_calls_refuse():
     assert _code(speculate.verify_drafts, *args) == INV    # on the CPU
     assert _code(speculate.verify_drafts, h, *args[1:]) == UNS
     assert _code(speculate.verify_drafts, *args[:2], i.view(3, 1), *args[3:]) == INV
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """They would be cut to their low bits on the way into the library."""
+    long = torch.zeros(1, 1).expand((1 << 32) + 1, 1)
+    assert _code(int8.rows_of, long, "x") == UNS
+    assert _code(int8.rows_of, long.t(), "x") == UNS
+    assert _code(int8.rows_of, torch.zeros(2, 3, 0), "x") == INV
 
 
 def test_product_plans(tmp_path):

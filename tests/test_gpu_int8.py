@@ -141,6 +141,22 @@ def test_strides_and_addresses(m, n, k, dtype):
     assert torch.equal(int8.linear(x.contiguous(), int8.quantize(w)), y)
 
 
+@pytest.mark.parametrize("m", [3, 40, 300])
+def test_offsets_beyond_32_bits(m):
+    """Rows far apart: elements past 2^32 of the activations and of the result."""
+    k, n = 333, 80
+    ld = (1 << 32) // (m - 1) // 64 * 64 + 64
+    x = torch.empty(ld * (m - 1) + k, dtype=torch.bfloat16, device="cuda").as_strided((m, k), (ld, 1))
+    out = torch.empty(ld * (m - 1) + n, dtype=torch.float32,
+                      device="cuda").as_strided((m, n), (ld, 1))
+    x.copy_(_draw(m, m, k, "bf16"))
+    w = _draw(m + 1, n, k)
+    wq = int8.quantize(w)
+    ref = _reference(x, w)
+    _close(int8.product(int8.quantize(x), wq, out=out), ref, "f32")
+    _close(int8.linear(x, wq, torch.float32), ref, "f32")
+
+
 def test_leading_dimensions_and_empty():
     x, w = _draw(3, 24, 320, "bf16"), int8.quantize(_draw(4, 90, 320, "bf16"))
     y = int8.linear(x, w)

@@ -148,6 +148,35 @@ def test_probs_strides_and_in_place(vocab, dtype, out):
         assert torch.equal(wide[:, 3 + vocab:], before[:, 3 + vocab:])
 
 
+def test_probs_of_very_many_rows():
+    """More rows than one launch takes, of lengths for each kernel."""
+    for rows, vocab, dtype in ((65536 * 3, 2, "f32"), (70001, 40, "bf16"), (65600, 8200, "bf16")):
+        x = _logits(rows, rows, vocab, dtype)
+        t = torch.linspace(0.5, 2.0, rows, device="cuda")
+        y = speculate.token_probs(x, t)
+        some = torch.tensor([0, 1, 65534, 65535, 65536, rows - 1], device="cuda")
+        _probs_close(y[some], x[some], t[some], "f32")
+    y = speculate.token_probs(torch.zeros((1 << 24) + 3, 1, device="cuda"))
+    assert bool((y == 1).all())
+
+
+@pytest.mark.parametrize("vocab", [3, 700, 20000, 70000])
+@pytest.mark.parametrize("rows", [18, 130])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_beyond_32_bits(vocab, rows, dtype):
+    """Rows far apart: elements past 2^32 of the logits and the probabilities."""
+    ld = (1 << 32) // (rows - 2) // 64 * 64
+    x, y = (torch.empty(ld * (rows - 1) + vocab, dtype=TD[dtype], device="cuda")
+            .as_strided((rows, vocab), (ld, 1)) for _ in range(2))
+    x.copy_(_logits(vocab, rows, vocab, dtype))
+    speculate.token_probs(x, out=y)
+    _probs_close(y, x, None, dtype)
+    args = _drafts(vocab, [1] * (rows // 2), vocab, dtype)
+    x.copy_(args["p"])
+    y[:rows // 2].copy_(args["q"])
+    _check(args, p=x, q=y[:rows // 2])
+
+
 def test_probs_shapes():
     x = _logits(5, 24, 700)
     y = speculate.token_probs(x)
