@@ -266,6 +266,9 @@ constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 
 // DEPTH tiles ahead, and add their int32 sums in LDS (integer sums do not depend
 // on their order).
 //
+// Bound: HBM, the weights once. 1 x 8192 x 28672 takes 39.1 us with everything (235
+// MB, 6.0 TB/s), of which start, rows and end are 3.
+//
 // XT = float or bf16_t (one strip of at most kFusedRows rows): the rows come as the
 // caller has them [M, K] (row stride ldx) and every block quantises them itself:
 // first their scales, with the weights' first tiles under way, then a tile's values
@@ -412,6 +415,9 @@ void quant_stream_kernel(const void* __restrict__ A, int64_t ldx, int K,
 // fragments of its strips and k tile into registers PF steps ahead, and all MT
 // row strips' fragments of the step, which the WC waves of a part share, go once
 // per block straight into a ring in LDS.
+//
+// Bound: HBM. 64 x 128256 x 8192 into fp32 takes 158 us (1084 MB, 6.9 TB/s), 167 in
+// a profile of single calls.
 template <int MT, int NF, int WC, int PF, typename OutT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_skinny_kernel(const char* __restrict__ A, const float* __restrict__ sa,
@@ -596,14 +602,14 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(const int* __restrict
 // columns; while it does, half of the next stage's rows and the other half's (the
 // next stage's) columns come out of LDS, six fragments a half on 8 x 4 strips, so
 // that LDS is read evenly. KG = 2: two such groups of waves on a half of the k range
-// each, for tiles too few to give a CU two blocks. One barrier a stage publishes the copies of stage kt +
-// 1 and frees the slot of stage kt - 1.
+// each, for tiles too few to give a CU two blocks. One barrier a stage publishes
+// the copies of stage kt + 1 and frees the slot of stage kt - 1.
 //
-// Bound: power. 2048 x 57344 x 8192 takes 735 us (2.62 Pop/s; a library int8
-// product reaches 2.16 there) at 1.84 GHz with the matrix units busy two thirds of
-// the time; with operands of zeros, hence little switching, 587 us. Measured
-// against it: 4 x 2 waves 750 us, reads in bursts 741, v_mfma_i32_32x32x32_i8 894,
-// four waves of 128 x 128 827, a ring of 5 759.
+// Bound: power. 2048 x 57344 x 8192 takes 735 us (2.62 Pop/s; up to 760 on other
+// cards; a library int8 product of 8192^3 reaches 2.16) at 1.84 GHz with the matrix
+// units busy two thirds of the time; with operands of zeros, hence little switching,
+// 587 us. Measured against it: 4 x 2 waves 750 us, reads in bursts 741,
+// v_mfma_i32_32x32x32_i8 894, four waves of 128 x 128 827, a ring of 5 759.
 template <int BM, int BN, int WM, int WN, int R, int KG, typename OutT>
 __global__ __launch_bounds__(KG * WM * WN * 64, 2) void quant_tiled_kernel(
     const char* __restrict__ A, const float* __restrict__ sa, const char* __restrict__ B,

@@ -2,9 +2,10 @@
 // code (no HIP calls).
 //
 // The candidates' times are estimated and the least is taken. The estimate has
-// three parts, in us, with constants fitted to 2100 timings of 126 sizes (1 to 3000
-// rows, 64 to 57344 columns, k of 128 to 28672); over those sizes the choice is
-// on average 1.2% and at worst 13% slower than the fastest candidate:
+// three parts, in us, with constants fitted to timings of 127 sizes (1 to 2958
+// rows, 67 to 128256 columns, k of 145 to 28672); over those sizes the choice is
+// on average 2.9% and at worst 23% (8 x 1280 x 8192: 8.6 against 7.0) slower than
+// the fastest of all kernels, range counts and tilings that were timed:
 //  - reading the operands from HBM at the rate that the kernel reaches;
 //  - what one CU has to load (few rows) or multiply (tiles) for its share of the
 //    blocks, which is what decides among them;
