@@ -603,7 +603,9 @@ __global__ __launch_bounds__(256) void quant_finish_kernel(const int* __restrict
 // next stage's) columns come out of LDS, six fragments a half on 8 x 4 strips, so
 // that LDS is read evenly. KG = 2: two such groups of waves on a half of the k range
 // each, for tiles too few to give a CU two blocks. One barrier a stage publishes
-// the copies of stage kt + 1 and frees the slot of stage kt - 1.
+// the copies of stage kt + 1 and frees the slot of stage kt - 1. Deeper rings gain
+// nothing (150 x 10240 x 5120 on 4 x 8 with 6, 9, 12 slots: 21.0, 21.0, 21.6 us): it
+// is what a CU takes in that bounds small tiles.
 //
 // Bound: power. 2048 x 57344 x 8192 takes 735 us (2.62 Pop/s; up to 760 on other
 // cards; a library int8 product of 8192^3 reaches 2.16) at 1.84 GHz with the matrix
@@ -653,8 +655,7 @@ __global__ __launch_bounds__(KG * WM * WN * 64, 2) void quant_tiled_kernel(
     const size_t strip = f < BM ? min(m0 + f, ms - 1) : min(n0 + f - BM, ns - 1);
     src[p] = (f < BM ? A : B) + (strip * KT + k0) * 1024;
   }
-  auto issue = [&](int kt) {
-    const int slot = kt % R;
+  auto issue = [&](int kt, int slot) {
     kt = kt < kts ? kt : kts - 1;  // past the end: into a slot that nobody reads
 #pragma unroll
     for (int p = 0; p < PW; ++p)
@@ -683,6 +684,10 @@ __global__ __launch_bounds__(KG * WM * WN * 64, 2) void quant_tiled_kernel(
       for (int j = 0; j < TH; ++j) acc[i][h * TH + j] = mfma_i8(b[j], a[i], acc[i][h * TH + j]);
   };
   u32x4_t a0[TM], a1[TM], b0[TH], b1[TH], bh[TH];
+  // Stage kt's slot: counted where R is no power of two (kt % R cost tiles of 4 x 8 and
+  // 8 x 8 up to 8%), else masked (counted, tiles of 4 x 4 lost 3%).
+  constexpr bool kCount = (R & (R - 1)) != 0;
+  int counted = 0;
   auto stage = [&](int kt, u32x4_t (&a)[TM], u32x4_t (&b)[TH], u32x4_t (&an)[TM],
                    u32x4_t (&bn)[TH]) {
     // this wave's copies of stage kt + 1 have landed; after the barrier all have
@@ -690,19 +695,22 @@ __global__ __launch_bounds__(KG * WM * WN * 64, 2) void quant_tiled_kernel(
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    issue(kt + R - 1);
+    const int slot = kCount ? counted : kt % R;
+    const int next = !kCount ? (kt + 1) % R : slot + 1 < R ? slot + 1 : 0;
+    issue(kt + R - 1, !kCount ? (kt + R - 1) % R : slot > 0 ? slot - 1 : R - 1);
     __builtin_amdgcn_sched_barrier(0);
-    read_b(bh, kt % R, 1);
-    read_a(an, (kt + 1) % R, 0);
+    read_b(bh, slot, 1);
+    read_a(an, next, 0);
     multiply(a, b, 0);
     __builtin_amdgcn_sched_barrier(0);
-    read_a(an, (kt + 1) % R, 1);
-    read_b(bn, (kt + 1) % R, 0);
+    read_a(an, next, 1);
+    read_b(bn, next, 0);
+    counted = next;
     multiply(a, bh, 1);
     __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
-  for (int t = 0; t < R - 1; ++t) issue(t);
+  for (int t = 0; t < R - 1; ++t) issue(t, t);
   __builtin_amdgcn_s_waitcnt(vmcnt_at_most((R - 2) * PW));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");

@@ -42,8 +42,8 @@ struct Tile {
 };
 constexpr Tile kTiles[] = {{QUANT_TILE_16X16, 16, 16, 4, 0.75, 0.0, 0.0},
                            {QUANT_TILE_12X8, 12, 8, 4, 0.31, 0.66, 1.0},
-                           {QUANT_TILE_8X8, 8, 8, 5, 0.22, 0.51, 1.1},
-                           {QUANT_TILE_4X8, 4, 8, 6, 0.137, 0.36, 0.9},
+                           {QUANT_TILE_8X8, 8, 8, 5, 0.212, 0.50, 1.1},
+                           {QUANT_TILE_4X8, 4, 8, 6, 0.129, 0.34, 0.9},
                            {QUANT_TILE_4X4, 4, 4, 8, 0.087, 0.22, 0.8}};
 struct Skinny {
   QuantKernel kind;
