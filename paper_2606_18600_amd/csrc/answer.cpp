@@ -3,6 +3,7 @@
 // here, before anything is enqueued.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
 
@@ -136,7 +137,10 @@ stage_status stage_quant_product(const void* a, int32_t m, const void* b, int32_
 size_t stage_quant_linear_bytes(int32_t m, int32_t n, int32_t k) {
   if (m < 1 || n < 1 || check_matrix(m, k, "x") != STAGE_OK || check_matrix(n, k, "w") != STAGE_OK)
     return 0;
-  return quant_linear_bytes(quant_plan(m, n, k, SIZE_MAX, true), m, n, k);
+  // for rows of either type
+  const size_t b16 = quant_linear_bytes(quant_plan(m, n, k, SIZE_MAX, 2), m, n, k);
+  const size_t f32 = quant_linear_bytes(quant_plan(m, n, k, SIZE_MAX, 4), m, n, k);
+  return std::max(b16, f32);
 }
 
 stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, int32_t m, int32_t k,
@@ -152,7 +156,7 @@ stage_status stage_quant_linear(stage_dtype dtype, const void* x, int64_t ld, in
   if ((v = check_rows(x, ld, k, esize(d), "x")) != STAGE_OK) return v;
   if ((v = check_packed(w, "w")) != STAGE_OK) return v;
   if ((v = check_rows(out, ldo, n, esize(o), "out")) != STAGE_OK) return v;
-  const QuantPlan plan = quant_plan(m, n, k, SIZE_MAX, true);
+  const QuantPlan plan = quant_plan(m, n, k, SIZE_MAX, (int)esize(d));
   if ((v = check_workspace(ws, ws_bytes, quant_linear_bytes(plan, m, n, k))) != STAGE_OK) return v;
   return launched("quant_linear", quant_linear(plan, (DType)d, x, ld, m, w, n, k, (DType)o, out,
                                                ldo, ws, (hipStream_t)stream));

@@ -68,9 +68,9 @@ struct QuantPlan {
   bool fused = false;
 };
 constexpr int kFusedRows = 4;
-// The plan of a product whose planes may take `room` bytes; with `rows`, of rows
-// that are still to be quantised.
-QuantPlan quant_plan(int M, int N, int K, size_t room, bool rows = false);
+// The plan of a product whose planes may take `room` bytes; with x_bytes, of rows
+// that are still to be quantised, from values of so many bytes.
+QuantPlan quant_plan(int M, int N, int K, size_t room, int x_bytes = 0);
 size_t quant_plane_bytes(const QuantPlan& p, int M, int N);
 // out [M, N] (fp32 or bf16, row stride ldo) = a b^T for the 8-bit matrices a
 // [M, K] and b [N, K]; planes: quant_plane_bytes() bytes.

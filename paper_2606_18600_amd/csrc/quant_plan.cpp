@@ -17,12 +17,12 @@
 //   skinny, 4 x 2       150 x 8192 x 28672     56.9 (skinny 4 x 4, 8 ranges: 58.2)
 //   skinny, 4 x 4       64 x 57344 x 8192      76.8 (skinny 4 x 2: 86.8)
 //   skinny, 4 x 8       64 x 128256 x 8192    158.3 (skinny 4 x 4: 184.9)
-//   tiles, 4 x 4        613 x 1277 x 2503       8.8 (tiles of 4 x 8: 11.6)
-//   ... two parts of k  256 x 4096 x 4096       9.3 (tiles of 4 x 4: 11.1)
-//   tiles, 4 x 8        150 x 10240 x 5120     20.4 (skinny 2 x 2: 24.4)
-//   tiles, 8 x 8        2048 x 2048 x 2048     12.6 (tiles of 4 x 8: 14.2)
-//   tiles, 12 x 8       2204 x 2560 x 5120     32.4 (tiles of 8 x 8: 40.5)
-//   tiles, 16 x 16      2048 x 57344 x 8192     735 (tiles of 8 x 8: 958)
+//   tiles, 4 x 4        529 x 1004 x 80         -
+//   ... two parts of k  256 x 4096 x 4096       9.1 (tiles of 4 x 4: 10.9)
+//   tiles, 4 x 8        200 x 5120 x 5120      14.6 (without: 15.5)
+//   tiles, 8 x 8        2048 x 2048 x 2048     12.0 (without: 15.3)
+//   tiles, 12 x 8       2204 x 2560 x 5120     30.9 (without: 40.5)
+//   tiles, 16 x 16      2048 x 57344 x 8192     741 (tiles of 12 x 8: 887)
 #include <algorithm>
 
 #include "answer.hpp"
@@ -62,7 +62,7 @@ size_t quant_plane_bytes(const QuantPlan& p, int M, int N) {
   return p.ranges > 1 ? (size_t)p.ranges * M * quant_rows16(N) * 4 : 0;
 }
 
-QuantPlan quant_plan(int M, int N, int K, size_t room, bool unquantised) {
+QuantPlan quant_plan(int M, int N, int K, size_t room, int x_bytes) {
   const long strips = up(N, 16), tiles = up(M, 16), KT = (long)quant_kp(K) / 64;
   const double mb = ((double)N * K + (double)M * K + (double)M * N * 2) * 1e-6;
   const double weights = (double)N * K;
@@ -81,17 +81,29 @@ QuantPlan quant_plan(int M, int N, int K, size_t room, bool unquantised) {
     }
     if (us < least) least = us, best = p;
   };
-  if (unquantised && M <= kFusedRows) {
-    // One launch that quantises the rows on the way, against 4 us for a launch of
-    // its own (1 x 8192 x 28672 on 1, 2, 3 strips a block: 48.1, 39.6, 41.9 us in all;
-    // 1 x 8192 x 8192 17.5, 16.3, 15.1; 1 x 1280 x 8192 10.5, 11.5, 12.9).
-    for (int nf : {1, 2, 3}) {
-      const long blocks = up(strips, nf), rounds = up(blocks, kCus);
-      offer(kStream[nf - 1], KT,
-            std::max(mb / 6.6, rounds * KT * nf / 34.0) + 0.28 * rounds +
-                0.014 * std::min<long>(blocks, kCus) - 4.0,
-            true);
+  if (x_bytes > 0 && M <= kFusedRows) {
+    // One launch that quantises the rows on the way, in place of two. A block of it
+    // reads every row and then a part of k per wave at 0.47 us a k tile; the launch
+    // that it saves takes the GPU about 5 us with its rows, and in short calls the
+    // host 3.8 us more, of which a captured graph sees none: half of that counts. One
+    // bf16 row, us from a stream (from a graph): 512 x 256 8.5 (3.6) against 12.3
+    // (4.9), 4096 x 4096 8.6 (8.0) against 12.4 (7.9), 8192 x 28672 39.2 against 43.4;
+    // 128256 x 8192 157 against 154; four fp32 rows of that 200 against 156. (Strips a
+    // block, 1, 2, 3: 1 x 8192 x 28672 48.1, 39.6, 41.9; 1 x 8192 x 8192 17.5, 16.3,
+    // 15.1; 1 x 1280 x 8192 10.5, 11.5, 12.9.)
+    int nf = 1;
+    double t = 1e30;
+    for (int f : {1, 2, 3}) {
+      const long blocks = up(strips, f), rounds = up(blocks, kCus);
+      const double us = std::max(mb / 6.6, rounds * KT * f / 34.0) + 0.28 * rounds +
+                        0.014 * std::min<long>(blocks, kCus);
+      if (us < t) t = us, nf = f;
     }
+    const long blocks = up(strips, nf), rounds = up(blocks, kCus), pairs = up(blocks, 2 * kCus);
+    const double row = M * (0.53 + 1.15e-5 * K * x_bytes);
+    const double us = 2.3 + pairs * (0.7 + row) +
+                      std::max({mb / 6.6, rounds * KT * nf / 34.0, KT * 0.059});
+    offer(kStream[nf - 1], KT, us - 5.2 - std::min(std::max(0.5 * (12.3 - us), 0.0), 1.9), true);
   }
   if (tiles <= kStreamStrips)
     for (int nf : {1, 3}) {

@@ -22,14 +22,14 @@ void check(bool ok, const char* what, int M, int N, int K, const QuantPlan& p) {
 
 long up(long a, long b) { return (a + b - 1) / b; }
 
-void check_plan(int M, int N, int K, size_t room, bool rows) {
-  const QuantPlan p = quant_plan(M, N, K, room, rows);
+void check_plan(int M, int N, int K, size_t room, int x_bytes) {
+  const QuantPlan p = quant_plan(M, N, K, room, x_bytes);
   const long KT = (long)quant_kp(K) / 64, strips = up(N, 16), tiles = up(M, 16);
   check(p.ranges >= 1 && p.kt_len >= 1, "empty plan", M, N, K, p);
   check((long)p.kt_len * p.ranges >= KT && (long)p.kt_len * (p.ranges - 1) < KT, "ranges", M, N, K,
         p);
   check(quant_plane_bytes(p, M, N) <= room, "room", M, N, K, p);
-  check(!p.fused || (rows && M <= kFusedRows && p.kernel <= QUANT_STREAM_3), "fused", M, N, K, p);
+  check(!p.fused || (x_bytes > 0 && M <= kFusedRows && p.kernel <= QUANT_STREAM_3), "fused", M, N, K, p);
   check(p.fused || p.kernel != QUANT_STREAM_2, "two strips", M, N, K, p);
   int bn = 1, kp = 2;
   switch (p.kernel) {
@@ -67,7 +67,7 @@ int main() {
     if (i % 5 == 0) M = edge[rng() % 13];
     if (i % 7 == 0) N = edge[rng() % 13];
     if (i % 11 == 0) K = edge[rng() % 12];
-    check_plan(M, N, K, i % 3 == 0 ? (size_t)draw(1, 1 << 28) : SIZE_MAX, i % 2 == 0);
+    check_plan(M, N, K, i % 3 == 0 ? (size_t)draw(1, 1 << 28) : SIZE_MAX, i % 2 == 0 ? 0 : i % 4 == 1 ? 2 : 4);
   }
   std::printf("plans passed\n");
 }
