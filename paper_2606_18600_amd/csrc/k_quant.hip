@@ -99,11 +99,13 @@ __device__ __forceinline__ u32x4_t quantise16(const V& v, float inv) {
 }
 
 // A block takes ROWS rows, 512 / ROWS threads to a row: thread tau row tau %
-// ROWS, 16-value chunks tau / ROWS + (512 / ROWS) c. With 8 rows a store
-// instruction covers whole 128-byte lines of the packed layout (8 rows x 16
-// bytes); one row per block gives few rows their parallelism. HELD chunks of a
-// thread stay in registers between the maximum and the rounding (8 rows of 8192:
-// all of them), the others are read twice.
+// ROWS, 16-value chunks tau / ROWS + (512 / ROWS) c. With 4 rows a store
+// instruction covers 64 adjacent bytes of the packed layout for each chunk; one row
+// per block gives few rows their parallelism. HELD chunks of a thread stay in
+// registers between the maximum and the rounding, the others are read twice.
+//
+// Bound: latency, then HBM: 64 rows of 8192 bf16 values take 3.2 us, 2048 11.1 (4.5
+// TB/s).
 template <typename T, int ROWS, int HELD>
 __global__ __launch_bounds__(512) void quant_rows_kernel(const T* __restrict__ src, int64_t ld,
                                                          int rows, int K, int KT,
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(256) void quant_pack_kernel(const int8_t* __restric
                                                          float* __restrict__ scales) {
   const int64_t total = (int64_t)rows * KT * 4, step = (int64_t)gridDim.x * 256;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
-    // 8 rows a turn, so that a wave's stores fill lines (as above)
+    // 8 rows a turn, so that a wave's stores fill lines of 128 bytes
     const int64_t per = (int64_t)KT * 4 * 8, g = i / per;
     const int in = (int)min<int64_t>(8, rows - g * 8);  // rows of this turn
     const int j = (int)(i - g * per);
@@ -908,12 +910,15 @@ template <typename T>
 hipError_t launch_quant_rows(const T* src, int64_t ld, int rows, int K, char* dst, float* scales,
                              hipStream_t s) {
   const int KT = (int)(quant_kp(K) / 64);
-  // 2048 rows of 8192 bf16 values 17.8 -> 11.7 us (4.3 TB/s), 613 of 2503 fp32 6.1 ->
-  // 4.8; but 512 of 8192 6.5 -> 9.6, one block for every fourth CU
-  if (rows >= 1024 || (rows >= 512 && K <= 4096))
-    quant_rows_kernel<T, 8, 8><<<(rows + 7) / 8, 512, 0, s>>>(src, ld, rows, K, KT, dst, scales);
-  else
+  // us with 1, 2, 4 rows a block: 150 rows of 5120 bf16 values 3.3, 3.4, 4.2; 300 4.3,
+  // 3.6, 4.3; 613 5.8, 5.6, 5.0; 2048 11.9, 8.6, 8.0 (and with 8 9.1)
+  constexpr int HELD = sizeof(T) == 4 ? 4 : 8;
+  if (rows < 256)
     quant_rows_kernel<T, 1, 4><<<rows, 512, 0, s>>>(src, ld, rows, K, KT, dst, scales);
+  else if (rows < 512)
+    quant_rows_kernel<T, 2, 4><<<(rows + 1) / 2, 512, 0, s>>>(src, ld, rows, K, KT, dst, scales);
+  else
+    quant_rows_kernel<T, 4, HELD><<<(rows + 3) / 4, 512, 0, s>>>(src, ld, rows, K, KT, dst, scales);
   return hipGetLastError();
 }
 

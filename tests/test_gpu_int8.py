@@ -141,6 +141,15 @@ def test_strides_and_addresses(m, n, k, dtype):
     assert torch.equal(int8.linear(x.contiguous(), int8.quantize(w)), y)
 
 
+# rows around the numbers that a block takes at once, longer than its registers hold
+@pytest.mark.parametrize("m", [255, 256, 257, 511, 514, 1027])
+@pytest.mark.parametrize("k", [63, 9001, 40003])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_a_block(m, k, dtype):
+    x, w = _draw(m, m, k, dtype), _draw(k, 40, k, dtype)
+    _close(int8.linear(x, int8.quantize(w), torch.float32), _reference(x, w), "f32")
+
+
 @pytest.mark.parametrize("m", [3, 40, 300])
 def test_offsets_beyond_32_bits(m):
     """Rows far apart: elements past 2^32 of the activations and of the result."""
